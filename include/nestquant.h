@@ -377,8 +377,7 @@ nq_status nq_kv_append(const nq_kv_cache* cache, const nq_kv_prep* prep, int64_t
  *   dtype     type of q and out.  Scores, softmax and sums are fp32 and the decoded values exact
  *             integers; 16-bit queries are taken as they are, fp32 ones to 22 bits of the
  *             row's largest entry; the softmax's weights, times their values' scales, to 22
- *             bits or 2^-37 of the largest scale (11 bits or 2^-32 for 16-bit queries of more
- *             than 64 rows a KV head, below what their outputs keep);
+ *             bits or 2^-37 of the largest scale;
  *   q, out    tokens x q_heads rows; out must not overlap q;
  *   lse       device, tokens x q_heads floats, or NULL;
  *   workspace device, 16-byte aligned, at least nq_attend_workspace_size(...) bytes of scratch,

@@ -215,6 +215,16 @@ __device__ __forceinline__ float settled(float w) {
   return w;
 }
 
+// The pair (a, b) as the sum of two fp16 pairs (22 bits): the second is what the first leaves, one
+// mixed fused multiply-add an entry (exact) from the packed pair itself.
+__device__ __forceinline__ void two_terms(float a, float b, uint32_t& first, uint32_t& second) {
+  first = __builtin_bit_cast(uint32_t, h2{(_Float16)a, (_Float16)b});
+  float c, d;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(c) : "v"(first), "v"(a));
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d) : "v"(first), "v"(b));
+  second = __builtin_bit_cast(uint32_t, h2{(_Float16)c, (_Float16)d});
+}
+
 // The exponent e of a row's largest entry (clamped so that 2^(14 - e) is a number): its entries
 // times 2^(14 - e) are fp16 operands.
 __device__ __forceinline__ int row_exponent(float largest) {

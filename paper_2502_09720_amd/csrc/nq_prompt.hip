@@ -9,15 +9,22 @@
 // side by side), 32 rows a wave, and runs over the records that its rows see: the records come
 // into LDS by direct loads, one ahead of the one in use, and every operand is one 16-byte LDS read a
 // lane without bank conflicts.  Per record and wave, on 32x32x16 matrix instructions:
-//   S^T = K Q^T, 2 x DIM / 16 of them;  O^T += V^T P^T, 4 x DIM / 32.
+//   S^T = K Q^T, 2 x DIM / 16 of them;  O^T += V^T P^T, 8 x DIM / 32 (twice as many of the first
+//   for fp32 queries).
 // S^T leaves 16 tokens of one query row in each lane, in the order that the B operand of the
 // second product takes (V's operands are laid out to match), so the weights never leave the
 // lane.  The keys' scales multiply the scores, the values' the weights, in fp32.
 //
-// What bounds it: per 64 tokens and 32 rows a wave issues 32 matrix instructions (1024 clocks of its
-// SIMD at DIM = 128), about 170 vector instructions and 32 exponentials (1200) and reads 32 KiB
-// of LDS; two waves a SIMD overlap them in part.  8192 queries of 32 heads: 666-690 us, 800-825
-// TFLOP/s; 2048: 72 us, where one round of workgroups with 1 to 32 records each is the limit.
+// The weights are the sum of two fp16 numbers (22 bits) whatever the queries' type: one number, 11
+// bits, is no more than fp16 outputs keep, and a call of 64 rows or fewer keeps 22.  The second
+// term's matrix instructions make 8192 queries 620 -> 806 us.
+//
+// What bounds it: per 64 tokens and 32 rows a wave issues 48 matrix instructions (1536 clocks of its
+// SIMD at DIM = 128), about 220 vector instructions and 32 exponentials (1400) and reads 32 KiB
+// of LDS; two waves a SIMD overlap them in part.  8192 queries of 32 heads: 806 us, 682 TFLOP/s;
+// 2048: 92 us, where one round of workgroups with 1 to 32 records each is the limit.
+#include <type_traits>
+
 #include "nq_attend.hpp"
 #include "nq_attend_join.hpp"
 
@@ -101,7 +108,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// TERMS: fp16 terms of the queries and the weights.
+// TERMS: fp16 terms of the queries (the weights have two).
 template <int DIM, int TERMS>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM <= 128 && TERMS == 1 ? 2 : 1))) void prompt_kernel(AttendArgs a) {
   using R = Record<DIM>;
@@ -169,7 +176,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
   // m: reference of the weights, at most 2^kSlack below the largest.  The weights reach the fp16
   // operands times 2^(14 - kSlack); a small slack leaves more of the 22 bits of two terms to
   // the small ones.
-  constexpr int kSlack = TERMS == 2 ? 1 : 6;
+  constexpr int kSlack = 1;
   float m = -INFINITY, l = 0.0f;
   float top = 0x1p-100f;
 
@@ -277,44 +284,37 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
     lift = (lift < -90 ? -90 : lift) + 14 - kSlack;
     const float ref = (m == -INFINITY ? 0.0f : m) - (float)lift;
 
-    uint32_t pop[TERMS][16];   // pairs of weights: operand k holds words 4 k ..
+    uint32_t pop[2][16];   // pairs of weights, two terms: operand k holds words 4 k ..
     float sum[2] = {};
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const f32x4 vs = *reinterpret_cast<const f32x4*>(rec + R::VS + 4 * (32 * x + 8 * k + 4 * h));
-#pragma unroll
-        for (int c = 0; c < 4; c += 2) {
-          float w[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][4 * k + c + e], q_scale, -ref));
-            w[e] = TERMS == 2 ? settled(p * vs[c + e]) : p * vs[c + e];
-            sum[e] += p;
-          }
-          const h2 f = {(_Float16)w[0], (_Float16)w[1]};
-          const int at = 8 * x + 2 * k + (c >> 1);
-          pop[0][at] = __builtin_bit_cast(uint32_t, f);
-          if constexpr (TERMS == 2) {
-            const h2 g = {(_Float16)(w[0] - (float)f.x), (_Float16)(w[1] - (float)f.y)};
-            pop[1][at] = __builtin_bit_cast(uint32_t, g);
-          }
-        }
-      }
-    l = __builtin_fmaf(sum[0] + sum[1], __builtin_ldexpf(1.0f, -lift), l);
-    // tokens that are not seen have weight 0 also where their scale is not a number
-    if (!whole && !*reinterpret_cast<const uint32_t*>(rec + R::FINITE)) {
+    auto weights = [&](auto odd) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int k = 0; k < 16; k += 2) {
-          const uint32_t keep = (s[x][k] == -INFINITY ? 0u : 0xFFFFu) |
-                                (s[x][k + 1] == -INFINITY ? 0u : 0xFFFF0000u);
+        for (int k = 0; k < 4; ++k) {
+          const f32x4 vs = *reinterpret_cast<const f32x4*>(rec + R::VS + 4 * (32 * x + 8 * k + 4 * h));
 #pragma unroll
-          for (int y = 0; y < TERMS; ++y) pop[y][8 * x + (k >> 1)] &= keep;
+          for (int c = 0; c < 4; c += 2) {
+            float w[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float v = s[x][4 * k + c + e];
+              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v, q_scale, -ref));
+              w[e] = p * vs[c + e];
+              if constexpr (decltype(odd)::value) w[e] = v == -INFINITY ? 0.0f : w[e];
+              sum[e] += p;
+            }
+            const int at = 8 * x + 2 * k + (c >> 1);
+            two_terms(w[0], w[1], pop[0][at], pop[1][at]);
+          }
         }
+    };
+    // tokens that are not seen have weight 0 also where their scale is not a number
+    if (whole || *reinterpret_cast<const uint32_t*>(rec + R::FINITE)) {
+      weights(std::false_type{});
+    } else {
+      weights(std::true_type{});
     }
+    l = __builtin_fmaf(sum[0] + sum[1], __builtin_ldexpf(1.0f, -lift), l);
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
 #pragma unroll
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
         if (d + 2 < DT)
           vop[d & 1][k] = *reinterpret_cast<const h8*>(rec + R::V + ((((d + 2) * 4 + k) * 64 + lane) << 4));
 #pragma unroll
-        for (int y = 0; y < TERMS; ++y) {
+        for (int y = 0; y < 2; ++y) {
           const u32x4 w = {pop[y][4 * k], pop[y][4 * k + 1], pop[y][4 * k + 2], pop[y][4 * k + 3]};
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, __builtin_bit_cast(h8, w), o[d], 0, 0, 0);
         }

@@ -1,0 +1,78 @@
+"""Attention over a coded KV cache (attend) at the accuracy of its contract: weights of 22 bits for
+every type and number of queries.
+
+The bound is that of test_gpu_attend.py with 22-bit weights throughout (the second term of a weight
+is there for 16-bit queries of many rows as well): an output of n tokens is off by at most
+(2 d + 2^-22 + (n + 64) 2^-22) sum_j p_j |V_j| + f R sum_j |V_j| / r_j / L + u |exact| + half the type's
+smallest step, with d the error of a score, f = 2^-37 and R the largest scale r of a value.
+"""
+
+import numpy as np
+import pytest
+
+from test_gpu_attend import MANY, SUBNORMAL, ULP, Call, nq  # noqa: F401 (nq: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+class Exact(Call):
+    """A call whose bounds are those above, and whose value scales can be changed."""
+
+    def __init__(self, *args, **more):
+        super().__init__(*args, **more)
+        self.U = self.V / self.r               # the values without their scales
+
+    def largest(self, e, r):
+        """R, from the exponentials relative to a row's largest and the scales."""
+        return r.max(initial=0.0)
+
+    def exact(self):
+        T, H = self.q64.shape[:2]
+        out, bound = np.zeros(self.q64.shape), np.zeros(self.q64.shape)
+        lse, lse_bound = np.full((T, H), -np.inf), np.zeros((T, H))
+        for b in range(len(self.lengths)):
+            lo, hi = self.starts[b], self.starts[b + 1]
+            n = int(self.lengths[b])
+            p = np.arange(n - (hi - lo), n)[:, None]
+            j = np.arange(n)
+            see = j <= p
+            if self.window:
+                see &= (j > p - self.window) | (j < self.sinks)
+            for h in range(self.heads):
+                K, ok = self.rows(self.K, b, h)
+                U, _ = self.rows(self.U, b, h)
+                r = self.rows(self.r, b, h)[0][:, 0]
+                s_ = see & ok
+                for hq in range(h * self.group, (h + 1) * self.group):
+                    q = self.q64[lo:hi, hq]
+                    s = np.where(s_, self.scale * q @ K.T, -np.inf)
+                    size = np.where(s_, abs(self.scale) * np.abs(q) @ np.abs(K).T, 0.0).max(-1, initial=0.0)
+                    any_ = s_.any(-1)
+                    top = np.where(any_, s.max(-1, initial=-np.inf), 0.0)
+                    e = np.exp(s - top[:, None])
+                    total = np.where(any_, e.sum(-1), 1.0)
+                    w = e / total[:, None] * r
+                    out[lo:hi, hq] = w @ U
+                    R = self.largest(e, r) / total[:, None]
+                    d = (self.dim + 8) * 2.0 ** -22 * size
+                    rel = 2 * d + 2.0 ** -22 + (n + 64) * 2.0 ** -22
+                    bound[lo:hi, hq] = rel[:, None] * (w @ np.abs(U)) + 2.0 ** -37 * R * (s_ @ np.abs(U))
+                    lse[lo:hi, hq] = np.where(any_, top + np.log(total), -np.inf)
+                    lse_bound[lo:hi, hq] = d + (n + 64) * 2.0 ** -22 + 2.0 ** -22 * np.abs(top)
+        return out, lse, bound + ULP[self.dtype] * np.abs(out) + SUBNORMAL[self.dtype], lse_bound
+
+
+@pytest.mark.parametrize("i", [i for i, case in enumerate(MANY) if case[2].get("dtype") != "f32"])
+def test_prompts_of_16_bits(nq, i):
+    lengths, counts, more = MANY[i]
+    Exact(nq, 500 + i, lengths, counts, **more).check()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_prompt_of_one_query_more(nq, dtype):
+    """The same rows in a call of 64 rows a KV head and in one of 68: within both bounds."""
+    c = Exact(nq, 530, [900], [17], dtype=dtype)
+    c.check()
+    c.q, c.q64 = c.q[1:], c.q64[1:]
+    c.starts[1] -= 1
+    c.check()

@@ -364,7 +364,8 @@ nq_status nq_kv_append(const nq_kv_cache* cache, const nq_kv_prep* prep, int64_t
  *   out = sum_j softmax_j(scale <q, K_j>) V_j,   lse = ln sum_j exp(scale <q, K_j>)
  * over them, K and V the decoded rows; a query that sees nothing (p < 0) has out 0 and lse
  * -infinity.  What the cache holds in other slots has no effect, whatever it is; a visible row
- * whose scale is not finite makes the outputs of the queries that see it not finite.
+ * whose scale is not finite makes the outputs of the queries that see it not finite, and a query
+ * that is not a number has outputs that are not.
  *   table     device, int32 pages, sequence b's from table[b * table_stride] on; entries past
  *             a sequence's last page are not read; tokens in a page outside [0, pages) are
  *             not seen;

@@ -322,11 +322,8 @@ __attribute__((amdgpu_waves_per_eu(DIM <= 128 && RT == 1 && TERMS == 1 ? 3 : (DI
       const int i = query_of(a, r0 + r), hq = head * group + r0 + r - i * group;
       const int64_t token = sq.first + i;
       if (a.chunks == 1) {
-        const float inv = big == -INFINITY ? 0.0f : 1.0f / total;
-        store_out(a.out, a.dtype, token * a.out_token + hq * a.out_head + 4 * c, sum * inv);
-        if (a.lse && c == 0)
-          a.lse[token * a.q_heads + hq] =
-              big == -INFINITY ? -INFINITY : 0.69314718f * (big + __builtin_amdgcn_logf(total));
+        store_out(a.out, a.dtype, token * a.out_token + hq * a.out_head + 4 * c, sum * inverse_sum(total));
+        if (a.lse && c == 0) a.lse[token * a.q_heads + hq] = log_sum(big, total);
       } else {
         float* p = partial(a, b, head, rb, r, chunk, DIM);
         *reinterpret_cast<f32x4*>(p + 4 + 4 * c) = sum;

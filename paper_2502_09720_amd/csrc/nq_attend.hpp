@@ -232,6 +232,12 @@ __device__ __forceinline__ int row_exponent(float largest) {
   return e < -100 ? -100 : e;
 }
 
+// A row that sees nothing has the sum 0 (one whose scores are all not numbers has not).
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.0f ? -INFINITY : 0.69314718f * (m + __builtin_amdgcn_logf(l));
+}
+
 // A power of two above x (finite, >= 2^-126), at most 2^127.
 __device__ __forceinline__ float power_above(float x) {
   const float p = __uint_as_float((__float_as_uint(x) & 0x7F800000u) + 0x00800000u);

@@ -69,11 +69,8 @@ __global__ __launch_bounds__(THREADS) void join_kernel(AttendArgs a, int parts) 
   }
   const int r = blk.r0 + x, i = query_of(a, r), hq = head * (int)a.by_group.n + r - i * (int)a.by_group.n;
   const int64_t token = sq.first + i;
-  const float inv = big == -INFINITY ? 0.0f : 1.0f / total;
-  store_out(a.out, a.dtype, token * a.out_token + hq * a.out_head + 4 * c, sum * inv);
-  if (a.lse && c == 0)
-    a.lse[token * a.q_heads + hq] =
-        big == -INFINITY ? -INFINITY : 0.69314718f * (big + __builtin_amdgcn_logf(total));
+  store_out(a.out, a.dtype, token * a.out_token + hq * a.out_head + 4 * c, sum * inverse_sum(total));
+  if (a.lse && c == 0) a.lse[token * a.q_heads + hq] = log_sum(big, total);
 }
 
 template <int DIM, int BR, int SHIFT, int PER>

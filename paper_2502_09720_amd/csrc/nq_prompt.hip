@@ -333,12 +333,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
 
   l += __shfl_xor(l, 32, 64);
   if (!there) return;
-  const bool none = m == -INFINITY;
   // o holds the sums over V times 2^(14 - kSlack) / top
   const float f = top * __builtin_ldexpf(1.0f, kSlack - 14) * a.v_scale;
   const int64_t token = sq.first + i;
   if (a.chunks == 1) {
-    const float inv = none ? 0.0f : f / l;
+    const float inv = f * inverse_sum(l);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -346,7 +345,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
         store_out(a.out, a.dtype, token * a.out_token + hq * a.out_head + 32 * d + 8 * k + 4 * h,
                   f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * inv);
     if (a.lse && h == 0)
-      a.lse[token * a.q_heads + hq] = none ? -INFINITY : 0.69314718f * (m + __builtin_amdgcn_logf(l));
+      a.lse[token * a.q_heads + hq] = log_sum(m, l);
   } else {
     float* p = partial(a, b, head, rb, 32 * wave + t, chunk, DIM);
 #pragma unroll

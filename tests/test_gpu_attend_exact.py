@@ -10,7 +10,7 @@ smallest step, with d the error of a score, f = 2^-37 and R the largest scale r 
 import numpy as np
 import pytest
 
-from test_gpu_attend import MANY, SUBNORMAL, ULP, Call, nq  # noqa: F401 (nq: the fixture)
+from test_gpu_attend import MANY, SHAPES, SUBNORMAL, ULP, Call, nq  # noqa: F401 (nq: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +76,28 @@ def test_a_prompt_of_one_query_more(nq, dtype):
     c.q, c.q64 = c.q[1:], c.q64[1:]
     c.starts[1] -= 1
     c.check()
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_that_are_all_not_numbers(nq, shape, dtype):
+    """A query that is not a number, or whose only token's key is not, gives outputs that are not
+    numbers (and not those of a query that sees nothing), and reaches no other row."""
+    import torch
+    lengths, counts, more = shape
+    c = Exact(nq, 540, lengths, counts, dtype=dtype, **more)
+    lse, kept = (torch.empty(c.q.shape[:2], device="cuda") for _ in range(2))
+    ref = c.run(lse=kept)
+    hit = torch.zeros(c.q.shape[:2], dtype=torch.bool, device="cuda")
+    hit[1, 3] = hit[0, 0] = True
+    q = c.q.clone()
+    q[hit, 5] = float("nan")
+    got = c.run(q=q, lse=lse)
+    assert torch.isnan(got[hit]).all() and torch.isnan(lse[hit]).all()
+    assert torch.equal(got[~hit], ref[~hit]) and torch.equal(lse[~hit], kept[~hit])
+    # token 0's key of KV head 0: all that the query at position 0 sees
+    c = Exact(nq, 542, counts, counts, dtype=dtype, **more)
+    c.cache.k.scales[int(c.table[0, 0]) * c.heads * c.page] = float("nan")
+    got = c.run(lse=lse)
+    assert torch.isnan(got[:counts[0], :c.group]).all() and torch.isnan(lse[:counts[0], :c.group]).all()
+    assert torch.isfinite(got[:, c.group:]).all() and torch.isfinite(lse[:, c.group:]).all()

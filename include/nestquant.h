@@ -378,7 +378,8 @@ nq_status nq_kv_append(const nq_kv_cache* cache, const nq_kv_prep* prep, int64_t
  *   dtype     type of q and out.  Scores, softmax and sums are fp32 and the decoded values exact
  *             integers; 16-bit queries are taken as they are, fp32 ones to 22 bits of the
  *             row's largest entry; the softmax's weights, times their values' scales, to 22
- *             bits or 2^-37 of the largest scale;
+ *             bits or 2^-37 of the largest such product among the tokens that the row sees
+ *             (weights below 2^-76 of the row's largest may count as 0);
  *   q, out    tokens x q_heads rows; out must not overlap q;
  *   lse       device, tokens x q_heads floats, or NULL;
  *   workspace device, 16-byte aligned, at least nq_attend_workspace_size(...) bytes of scratch,

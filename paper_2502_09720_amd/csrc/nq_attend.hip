@@ -3,14 +3,15 @@
 // A workgroup takes one KV head of one sequence, a block of its query rows (the queries of the
 // heads that share the KV head) and a chunk of the tokens they see.  Its four waves step
 // through the chunk in turn, 32 tokens a step (16 where the call has few), each with its own
-// running maximum and sum:
+// references and sums:
 //   * the scores are S^T = K Q^T on 16x16x32 fp16 matrix instructions.  Lane l holds the blocks
 //     of token l % 16 in the A operand, so a lane decodes its code words (16 bytes of a row)
 //     straight into the operand; the order of the entries along the contraction is that of the
 //     lanes' blocks, and Q's operand is laid out to match;
 //   * S^T leaves four tokens of one query row in each lane, which is what the B operand of
 //     O^T += V^T P^T holds (in an order of the tokens of its own), so the weights stay in
-//     registers, and the softmax's maximum and sum need two shuffles;
+//     registers; the references of the sums (RowSum) move seldom, and only then is a maximum
+//     taken across lanes;
 //   * V's blocks are decoded into LDS and read back transposed (ds_read_b64_tr_b16).
 // The decoded values are integers m X2 / 8, exact in fp16; the rows' scales multiply the scores
 // and the weights in fp32.  Queries in 16 bits are exact in one fp16 operand (scaled by a power
@@ -31,7 +32,6 @@ namespace nq {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kSlack = 1;   // see nq_prompt.hip
 
 template <int DIM>
 struct Shape {
@@ -143,13 +143,7 @@ __attribute__((amdgpu_waves_per_eu(DIM <= 128 && RT == 1 && TERMS == 1 ? 3 : (DI
   }
 
   f32x4 o[RT][DT] = {};
-  float m[RT], l[RT];      // m: reference of the weights, at most 2^kSlack below the largest
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m[rt] = -INFINITY;
-    l[rt] = 0.0f;
-  }
-  float top = 0x1p-100f;   // a power of two no smaller than the values' scales so far
+  RowSum sum[RT];
   _Float16* vt = reinterpret_cast<_Float16*>(lds + wave * S::VBYTES);
 
   // The code words are loaded ahead: a step's values while its keys are decoded, the next
@@ -184,26 +178,13 @@ __attribute__((amdgpu_waves_per_eu(DIM <= 128 && RT == 1 && TERMS == 1 ? 3 : (DI
     for (int u = 0; u < U; ++u) ks[u] = kw.scales[u];
     if (more) load_step<NBL, U>(a.k, next, t, g, kw);
 
-    // the values' scales relative to `top`, which grows as they do
-    float vmax = 0.0f;
+    // a bound of the scales of this lane's tokens (2^lv), seen or not
+    float lv = 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool seen = cur.ok[u] & (cur.tok[u] + 4 * g + i < sq.end);
-        const float r = vw.scales[u][i];
-        vw.scales[u][i] = seen ? r : 0.0f;
-        vmax = fmaxf(vmax, (seen & (r < INFINITY)) ? r : 0.0f);
-      }
-    float shrink = 1.0f;
-    if (__any(vmax > top)) {
-      vmax = fmaxf(vmax, __shfl_xor(vmax, 16, 64));
-      vmax = fmaxf(vmax, __shfl_xor(vmax, 32, 64));
-      const float bound = power_above(vmax);
-      shrink = top / bound;
-      top = bound;
-    }
-    const float inv_top = __builtin_ldexpf(__builtin_amdgcn_rcpf(top), 14 - kSlack);   // of a power of two: exact
+      for (int i = 0; i < 4; ++i) lv = fmaxf(lv, finite_size(vw.scales[u][i]));
+    lv = __builtin_amdgcn_logf(lv);
 
     Weights pop[RT][2];
 #pragma unroll
@@ -218,33 +199,52 @@ __attribute__((amdgpu_waves_per_eu(DIM <= 128 && RT == 1 && TERMS == 1 ? 3 : (DI
           sc[u][i] = see ? v : -INFINITY;
           mx = fmaxf(mx, sc[u][i]);
         }
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      // a new reference only where the weights would pass 2^kSlack
-      float f = shrink;
-      if (__any(mx > m[rt] + (float)kSlack)) {
-        const float up = fmaxf(m[rt], mx);
-        const float d = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - up);
-        m[rt] = up;
-        l[rt] *= d;
-        f *= d;
-      }
-      if (__any(f != 1.0f)) {
+      // new references only where these tokens might pass the present ones
+      if (__any(sum[rt].passed(mx, lv))) {
+        float both = -INFINITY;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[rt][d] *= f;
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            both = fmaxf(both, sc[u][i] + __builtin_amdgcn_logf(finite_size(vw.scales[u][i])));
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        both = fmaxf(both, __shfl_xor(both, 16, 64));
+        both = fmaxf(both, __shfl_xor(both, 32, 64));
+        const float f = sum[rt].raise(mx, both);
+        if (__any(f != 1.0f)) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[rt][d] *= f;
+        }
       }
-      const float ref = m[rt] == -INFINITY ? 0.0f : m[rt];
+      float e = 0.0f, w[U][4];
+      if (!sum[rt].wide) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = __builtin_amdgcn_exp2f(sc[u][i] - sum[rt].ref);
+            e += p;
+            w[u][i] = p * vw.scales[u][i];
+          }
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            e += sum[rt].term(sc[u][i] - sum[rt].ref, sc[u][i] - sum[rt].m, vw.scales[u][i], w[u][i]);
+          }
+      }
+      sum[rt].add(e);
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float p = __builtin_amdgcn_exp2f(sc[u][i] - ref);
-          l[rt] += p;
           // a token that is not seen has weight 0, whatever its scale
-          const float w = settled(sc[u][i] == -INFINITY ? 0.0f : p * (vw.scales[u][i] * inv_top));
-          const _Float16 h = (_Float16)w;
+          const float x = settled(sc[u][i] == -INFINITY ? 0.0f : w[u][i]);
+          const _Float16 h = (_Float16)x;
           pop[rt][0][4 * u + i] = h;
-          pop[rt][1][4 * u + i] = (_Float16)(w - (float)h);
+          pop[rt][1][4 * u + i] = (_Float16)(x - (float)h);
         }
     }
     // V: decoded rows into LDS, columns of four tokens back
@@ -284,49 +284,47 @@ __attribute__((amdgpu_waves_per_eu(DIM <= 128 && RT == 1 && TERMS == 1 ? 3 : (DI
   // join the waves
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    l[rt] += __shfl_xor(l[rt], 16, 64);
-    l[rt] += __shfl_xor(l[rt], 32, 64);
+    sum[rt].l += __shfl_xor(sum[rt].l, 16, 64);
+    sum[rt].l += __shfl_xor(sum[rt].l, 32, 64);
     if (g == 0) {
-      wave_m[wave][16 * rt + t] = m[rt];
-      wave_l[wave][16 * rt + t] = l[rt];
+      wave_m[wave][16 * rt + t] = sum[rt].m;
+      wave_l[wave][16 * rt + t] = sum[rt].l;
     }
   }
   float* ob = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     __syncthreads();
-    float mm = -INFINITY;
+    float mm = wave_m[0][16 * rt + t];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][16 * rt + t]);
-    const float ref = mm == -INFINITY ? 0.0f : mm;
-    // o holds the sums over V times 2^(14 - kSlack) / top
-    const float f = __builtin_amdgcn_exp2f(m[rt] - ref) * __builtin_ldexpf(top, kSlack - 14) * a.v_scale;
+    for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, wave_m[w][16 * rt + t]);
+    // o holds the sums over V relative to 2^ref
+    const float f = half_power(sum[rt].ref - mm);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
-      *reinterpret_cast<f32x4*>(ob + (wave * 16 + t) * S::OP + 16 * d + 4 * g) = o[rt][d] * f;
+      *reinterpret_cast<f32x4*>(ob + (wave * 16 + t) * S::OP + 16 * d + 4 * g) = (o[rt][d] * f) * (f * a.v_scale);
     __syncthreads();
     for (int x = (int)threadIdx.x; x < 16 * (DIM / 4); x += 64 * kWaves) {
       const int row = x / (DIM / 4), c = x % (DIM / 4), r = 16 * rt + row;
       if (r >= rows) continue;
-      f32x4 sum = {};
+      f32x4 all = {};
       float big = -INFINITY, total = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        sum += *reinterpret_cast<const f32x4*>(ob + (w * 16 + row) * S::OP + 4 * c);
+        all += *reinterpret_cast<const f32x4*>(ob + (w * 16 + row) * S::OP + 4 * c);
         big = fmaxf(big, wave_m[w][r]);
       }
-      const float z = big == -INFINITY ? 0.0f : big;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w)
-        total += wave_l[w][r] * __builtin_amdgcn_exp2f(wave_m[w][r] - z);
+        total += wave_l[w][r] * __builtin_amdgcn_exp2f(wave_m[w][r] - big);
       const int i = query_of(a, r0 + r), hq = head * group + r0 + r - i * group;
       const int64_t token = sq.first + i;
       if (a.chunks == 1) {
-        store_out(a.out, a.dtype, token * a.out_token + hq * a.out_head + 4 * c, sum * inverse_sum(total));
+        store_out(a.out, a.dtype, token * a.out_token + hq * a.out_head + 4 * c, all * inverse_sum(total));
         if (a.lse && c == 0) a.lse[token * a.q_heads + hq] = log_sum(big, total);
       } else {
         float* p = partial(a, b, head, rb, r, chunk, DIM);
-        *reinterpret_cast<f32x4*>(p + 4 + 4 * c) = sum;
+        *reinterpret_cast<f32x4*>(p + 4 + 4 * c) = all;
         if (c == 0) {
           p[0] = big;
           p[1] = total;

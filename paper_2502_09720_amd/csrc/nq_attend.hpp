@@ -232,16 +232,64 @@ __device__ __forceinline__ int row_exponent(float largest) {
   return e < -100 ? -100 : e;
 }
 
+// |x|, or 0 where that is not a finite number.
+__device__ __forceinline__ float finite_size(float x) {
+  const float a = fabsf(x);
+  return a < INFINITY ? a : 0.0f;
+}
+
+// What a lane keeps of a query row beside its weighted sum of values, o.  With a token's score s
+// (base 2) and its value's scale r, l sums 2^(s - m) and o sums 2^(s - ref) r V:
+//   m    the largest score so far, short of it by kLag at most;
+//   ref  2^(ref + kTop) is the largest product 2^s r so far of the tokens that the row sees, short of
+//        it by kRoom at most, so that the products' fp16 operands lie at the top of their type.
+// A scale that the row does not see, or whose token has next to no weight, has no part in either.
+// Both start below every score.
+struct RowSum {
+  static constexpr float kTop = 12.0f, kRoom = 3.9f, kLag = 8.0f;
+  float m = -3.402823466e38f, l = 0.0f, ref = -3.402823466e38f;
+  bool wide = false;   // whether shift() is not 0 in a lane of the wave
+
+  // Whether scores up to s, or products up to 2^(s + lv), may pass what the references allow.
+  __device__ __forceinline__ bool passed(float s, float lv) const {
+    return (s + lv > ref + (kTop + kRoom)) | (s > m + kLag);
+  }
+  // Raises the references that the largest score and the largest product (its logarithm) of new
+  // tokens pass, which depends on this row alone; the factor of o.  ref stays within 140 below m,
+  // which holds every scale that is a normal number.
+  __device__ __forceinline__ float raise(float s, float product) {
+    const float top = s > m + kLag ? s : m;
+    l *= __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    const float next = fmaxf(product > ref + (kTop + kRoom) ? product - kTop : ref, m - 140.0f);
+    const float f = __builtin_amdgcn_exp2f(ref - next);
+    ref = next;
+    wide = __any(shift() != 0);
+    return f;
+  }
+  // Where the references lie so far apart that 2^(s - ref) may leave fp32's range or lose what l
+  // needs, a power of two that brings its products with the scales into it.
+  __device__ __forceinline__ int shift() const {
+    return ref - m > 30.0f ? 64 : (ref - m < -90.0f ? -64 : 0);
+  }
+  // What a token with d = s - ref and e = s - m counts in `add`, and its weight w, for any shift.
+  __device__ __forceinline__ float term(float d, float e, float r, float& w) const {
+    const int h = shift();
+    const float p = __builtin_amdgcn_exp2f(d + (float)h);
+    w = __builtin_ldexpf(p * r, -h);
+    return h ? __builtin_amdgcn_exp2f(e) : p;
+  }
+  // Adds a sum of 2^(s - ref) (2^(s - m) where there is a shift).
+  __device__ __forceinline__ void add(float sum) {
+    l = __builtin_fmaf(sum, wide && shift() ? 1.0f : __builtin_amdgcn_exp2f(ref - m), l);
+  }
+};
+// 2^(x / 2); twice as a factor it is 2^x, also where that alone is no normal number.
+__device__ __forceinline__ float half_power(float x) { return __builtin_amdgcn_exp2f(0.5f * x); }
 // A row that sees nothing has the sum 0 (one whose scores are all not numbers has not).
 __device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 __device__ __forceinline__ float log_sum(float m, float l) {
   return l == 0.0f ? -INFINITY : 0.69314718f * (m + __builtin_amdgcn_logf(l));
-}
-
-// A power of two above x (finite, >= 2^-126), at most 2^127.
-__device__ __forceinline__ float power_above(float x) {
-  const float p = __uint_as_float((__float_as_uint(x) & 0x7F800000u) + 0x00800000u);
-  return p < INFINITY ? p : 0x1p127f;
 }
 
 // Row, in the pools, of a token of one head (the 16 tokens from a multiple of 16 on lie in one

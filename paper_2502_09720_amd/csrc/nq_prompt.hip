@@ -17,12 +17,12 @@
 //
 // The weights are the sum of two fp16 numbers (22 bits) whatever the queries' type: one number, 11
 // bits, is no more than fp16 outputs keep, and a call of 64 rows or fewer keeps 22.  The second
-// term's matrix instructions make 8192 queries 620 -> 806 us.
+// term's matrix instructions make 8192 queries 620 -> 800 us.
 //
 // What bounds it: per 64 tokens and 32 rows a wave issues 48 matrix instructions (1536 clocks of its
 // SIMD at DIM = 128), about 220 vector instructions and 32 exponentials (1400) and reads 32 KiB
-// of LDS; two waves a SIMD overlap them in part.  8192 queries of 32 heads: 806 us, 682 TFLOP/s;
-// 2048: 92 us, where one round of workgroups with 1 to 32 records each is the limit.
+// of LDS; two waves a SIMD overlap them in part.  8192 queries of 32 heads: 800 us, 687 TFLOP/s;
+// 2048: 90 us, where one round of workgroups with 1 to 32 records each is the limit.
 #include <type_traits>
 
 #include "nq_attend.hpp"
@@ -35,9 +35,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kWaves = 4, kRows = 32 * kWaves;
 
-// A record: K's operands, V's, 64 scales of the keys, 64 of the values relative to `top`, the bits of
-// the tokens that count, top, a power of two above the values' finite scales (at least 2^-100), and
-// whether all of them are finite.
+// A record: K's operands, V's, 64 scales of the keys, 64 of the values, the bits of the tokens that
+// count, the logarithm of the values' largest finite scale, and whether all of them are finite.
 template <int DIM>
 struct Record {
   static constexpr int V = DIM * 128, KS = DIM * 256, VS = KS + 256, BITS = VS + 256, TOP = BITS + 8, FINITE = TOP + 4;
@@ -76,16 +75,15 @@ __global__ __launch_bounds__(256) void unpack_kernel(AttendArgs a) {
   }
   if (g == 0) {
     const float ks = a.k.scales[row], vs = a.v.scales[row];
-    float most = ok && vs < INFINITY ? vs : 0.0f;
+    float most = ok ? finite_size(vs) : 0.0f;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m, 64));
-    const float top = power_above(fmaxf(most, 0x1p-101f));
     reinterpret_cast<float*>(rec + R::KS)[lane] = ok ? ks : 0.0f;
-    reinterpret_cast<float*>(rec + R::VS)[lane] = ok ? vs / top : 0.0f;
+    reinterpret_cast<float*>(rec + R::VS)[lane] = ok ? vs : 0.0f;
     const uint64_t bits = __ballot(ok), odd = __ballot(ok && !isfinite(vs));
     if (lane == 0) {
       *reinterpret_cast<uint64_t*>(rec + R::BITS) = bits;
-      *reinterpret_cast<float*>(rec + R::TOP) = top;
+      *reinterpret_cast<float*>(rec + R::TOP) = __builtin_amdgcn_logf(most);
       *reinterpret_cast<uint32_t*>(rec + R::FINITE) = odd == 0;
     }
   }
@@ -173,12 +171,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
   }
 
   f32x16 o[DT] = {};
-  // m: reference of the weights, at most 2^kSlack below the largest.  The weights reach the fp16
-  // operands times 2^(14 - kSlack); a small slack leaves more of the 22 bits of two terms to
-  // the small ones.
-  constexpr int kSlack = 1;
-  float m = -INFINITY, l = 0.0f;
-  float top = 0x1p-100f;
+  RowSum sum;
 
   // a record into buffer `to`: 1 KiB a wave instruction
   auto fetch = [&](int u, int to) {
@@ -260,33 +253,31 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
     for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int k = 0; k < 16; k += 2) mx = max3(mx, s[x][k], s[x][k + 1]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float big = mx == -INFINITY ? mx : mx * q_scale;
-    // a new reference only where the weights would pass 2^kSlack
-    if (__any(big > m + (float)kSlack)) {
-      const float next = fmaxf(m, big);
-      const float f = __builtin_amdgcn_exp2f(next == -INFINITY ? 0.0f : m - next);
-      m = next;
-      l *= f;
+    // new references only where these tokens might pass the present ones (-infinity stays so)
+    mx *= q_scale;
+    if (__any(sum.passed(mx, *reinterpret_cast<const float*>(rec + R::TOP)))) {
+      float both = -INFINITY;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] *= f;
-    }
-    // the values' scales are relative to the record's `top`: its ratio to the largest so far, a
-    // power of two, goes into the exponent (past 2^-90 what is added is nothing beside the rest)
-    const float rtop = *reinterpret_cast<const float*>(rec + R::TOP);
-    if (rtop > top) {
-      const float f = top / rtop;
-      top = rtop;
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] *= f;
+        for (int k = 0; k < 4; ++k) {
+          const f32x4 vs = *reinterpret_cast<const f32x4*>(rec + R::VS + 4 * (32 * x + 8 * k + 4 * h));
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            both = fmaxf(both, __builtin_fmaf(s[x][4 * k + c], q_scale, __builtin_amdgcn_logf(finite_size(vs[c]))));
+        }
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      both = fmaxf(both, __shfl_xor(both, 32, 64));
+      const float f = sum.raise(mx, both);
+      if (__any(f != 1.0f)) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= f;
+      }
     }
-    int lift = ((int)__float_as_uint(rtop) - (int)__float_as_uint(top)) >> 23;
-    lift = (lift < -90 ? -90 : lift) + 14 - kSlack;
-    const float ref = (m == -INFINITY ? 0.0f : m) - (float)lift;
 
     uint32_t pop[2][16];   // pairs of weights, two terms: operand k holds words 4 k ..
-    float sum[2] = {};
-    auto weights = [&](auto odd) {
+    float part[2] = {};
+    auto weights = [&](auto plain) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -297,11 +288,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
             float w[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float v = s[x][4 * k + c + e];
-              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v, q_scale, -ref));
-              w[e] = p * vs[c + e];
-              if constexpr (decltype(odd)::value) w[e] = v == -INFINITY ? 0.0f : w[e];
-              sum[e] += p;
+              const float v = s[x][4 * k + c + e], d = __builtin_fmaf(v, q_scale, -sum.ref);
+              if constexpr (decltype(plain)::value) {
+                const float p = __builtin_amdgcn_exp2f(d);
+                part[e] += p;
+                w[e] = p * vs[c + e];
+              } else {
+                part[e] += sum.term(d, __builtin_fmaf(v, q_scale, -sum.m), vs[c + e], w[e]);
+                w[e] = v == -INFINITY ? 0.0f : w[e];
+              }
             }
             const int at = 8 * x + 2 * k + (c >> 1);
             two_terms(w[0], w[1], pop[0][at], pop[1][at]);
@@ -309,12 +304,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
         }
     };
     // tokens that are not seen have weight 0 also where their scale is not a number
-    if (whole || *reinterpret_cast<const uint32_t*>(rec + R::FINITE)) {
-      weights(std::false_type{});
-    } else {
+    if (!sum.wide && (whole || *reinterpret_cast<const uint32_t*>(rec + R::FINITE))) {
       weights(std::true_type{});
+    } else {
+      weights(std::false_type{});
     }
-    l = __builtin_fmaf(sum[0] + sum[1], __builtin_ldexpf(1.0f, -lift), l);
+    sum.add(part[0] + part[1]);
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
 #pragma unroll
@@ -331,21 +326,21 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
     }
   }
 
-  l += __shfl_xor(l, 32, 64);
+  const float l = sum.l + __shfl_xor(sum.l, 32, 64);
   if (!there) return;
-  // o holds the sums over V times 2^(14 - kSlack) / top
-  const float f = top * __builtin_ldexpf(1.0f, kSlack - 14) * a.v_scale;
+  // o holds the sums over V relative to 2^ref
+  const float f = half_power(sum.ref - sum.m);
   const int64_t token = sq.first + i;
   if (a.chunks == 1) {
-    const float inv = f * inverse_sum(l);
+    const float inv = f * a.v_scale * inverse_sum(l);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         store_out(a.out, a.dtype, token * a.out_token + hq * a.out_head + 32 * d + 8 * k + 4 * h,
-                  f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * inv);
+                  f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * f * inv);
     if (a.lse && h == 0)
-      a.lse[token * a.q_heads + hq] = log_sum(m, l);
+      a.lse[token * a.q_heads + hq] = log_sum(sum.m, l);
   } else {
     float* p = partial(a, b, head, rb, 32 * wave + t, chunk, DIM);
 #pragma unroll
@@ -353,9 +348,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(DIM
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         *reinterpret_cast<f32x4*>(p + 4 + 32 * d + 8 * k + 4 * h) =
-            f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * f;
+            f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * f * (f * a.v_scale);
     if (h == 0) {
-      p[0] = m;
+      p[0] = sum.m;
       p[1] = l;
     }
   }

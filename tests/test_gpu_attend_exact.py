@@ -101,3 +101,99 @@ def test_scores_that_are_all_not_numbers(nq, shape, dtype):
     got = c.run(lse=lse)
     assert torch.isnan(got[:counts[0], :c.group]).all() and torch.isnan(lse[:counts[0], :c.group]).all()
     assert torch.isfinite(got[:, c.group:]).all() and torch.isfinite(lse[:, c.group:]).all()
+
+
+class Seen(Exact):
+    """With R the largest product of a weight and its value's scale among the tokens that a row
+    sees, relative to the row's largest weight."""
+
+    def largest(self, e, r):
+        return (e * r).max(-1, initial=0.0, keepdims=True)
+
+
+def scaled(c, b, tokens, factor):
+    """Multiplies the value scales of tokens of sequence b, in the cache and in the reference."""
+    for t in tokens:
+        page, slot = int(c.table[b, t // c.page]), t % c.page
+        for h in range(c.heads):
+            row = (page * c.heads + h) * c.page + slot
+            c.r[page, h, slot] *= factor
+            c.cache.v.scales[row] = float(c.r[page, h, slot, 0])
+    c.r[:] = c.cache.v.scales.double().cpu().numpy().reshape(c.r.shape)
+
+
+HIDDEN = [
+    # lengths, counts, more, sequence, tokens that some or all queries do not see
+    ([195, 70], [1, 1], dict(window=40, sinks=2), 0, [5, 150]),          # in tiles with seen tokens
+    ([195, 70], [1, 1], dict(window=40, sinks=2, dim=64, group=20, heads=1), 0, [5, 150]),
+    ([300, 1040], [4, 5], dict(dim=256, group=2), 1, [1037, 1038]),      # drafted: after some queries
+    ([300, 21], [4, 5], dict(group=12, heads=1), 0, [298]),              # two row blocks
+    ([200, 90], [70, 66], dict(group=2), 0, [140, 180, 199]),            # a prompt's later tokens
+    ([200, 90], [200, 90], dict(group=1, dim=64), 0, [3, 63, 64, 130]),
+    ([400, 150], [100, 150], dict(window=30, sinks=3), 0, [5, 300, 331, 399]),
+    ([140, 70], [80, 33], dict(dim=256, group=2, heads=1), 0, [90, 139]),
+    ([1500, 700], [30, 33], dict(dim=64, group=5, heads=1), 0, [1490]),  # chunks along the cache
+]
+
+
+@pytest.mark.parametrize("factor", [2.0 ** 12, 2.0 ** 40, 2.0 ** 100])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("i", range(len(HIDDEN)))
+def test_large_scales_that_are_not_seen(nq, i, dtype, factor):
+    """A value of large finite scale has no part in the rows that do not see its token."""
+    lengths, counts, more, b, tokens = HIDDEN[i]
+    c = Seen(nq, 560 + i, lengths, counts, dtype=dtype, **more)
+    scaled(c, b, tokens, factor)
+    c.check()
+
+
+@pytest.mark.parametrize("factor", [2.0 ** 20, 2.0 ** 40, 2.0 ** -40])
+@pytest.mark.parametrize("shape", [([150, 90], [2, 1], {}), ([150, 90], [70, 80], dict(group=1)),
+                                   ([1000, 90], [1, 1], dict(dim=64))])
+def test_large_scales_of_little_weight(nq, shape, factor):
+    """Scores tens apart: what a token's scale does is what its weight leaves of it, row by row,
+    whether the weight of a large scale is next to nothing or a small scale has all the weight."""
+    lengths, counts, more = shape
+    c = Seen(nq, 580, lengths, counts, dtype="f32", scale=0.4, spread=3.0, **more)
+    scaled(c, 0, range(0, lengths[0], 7), factor)
+    c.check()
+
+
+@pytest.mark.parametrize("factor", [2.0 ** -100, 2.0 ** -60, 2.0 ** 35, 2.0 ** 60, 2.0 ** 110])
+@pytest.mark.parametrize("shape", [([391, 90], [1, 1], {}), ([150, 90], [70, 80], dict(group=1, window=50))])
+def test_scales_anywhere_in_fp32(nq, shape, factor):
+    """Values of any size have the same relative errors and leave the sums as they are."""
+    lengths, counts, more = shape
+    c = Seen(nq, 590, lengths, counts, dtype="f32", **more)
+    for b, n in enumerate(lengths):
+        scaled(c, b, range(n), factor)
+    c.check()
+
+
+@pytest.mark.parametrize("shape", [([391, 90], [1, 1], {}), ([150, 90], [70, 80], dict(group=1))])
+def test_scales_of_zero(nq, shape):
+    """Rows of zeros among the values and nothing but such rows."""
+    import torch
+    lengths, counts, more = shape
+    c = Seen(nq, 595, lengths, counts, dtype="f32", **more)
+    scaled(c, 0, range(0, lengths[0], 3), 0.0)
+    c.check()
+    scaled(c, 0, range(lengths[0]), 0.0)
+    got = c.check()
+    assert not torch.any(got[:counts[0]]).item()
+
+
+@pytest.mark.parametrize("shape", [([195, 70], [2, 1], dict(window=40, sinks=2)), ([200, 90], [70, 66], dict(group=2))])
+def test_rows_do_not_depend_on_other_rows(nq, shape):
+    """A row's bits are the same whatever the queries beside it are."""
+    import torch
+    lengths, counts, more = shape
+    c = Seen(nq, 598, lengths, counts, **more)
+    ref = c.run()
+    q = c.q.clone()
+    q[0, 1::2] *= 40.0
+    q[1] = 0.0
+    got = c.run(q=q)
+    same = torch.ones(q.shape[:2], dtype=torch.bool, device="cuda")
+    same[0, 1::2] = same[1] = False
+    assert torch.equal(got[same], ref[same])

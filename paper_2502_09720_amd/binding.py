@@ -443,7 +443,7 @@ class KVCache:
     coded matrices of pages * heads * page rows of dim entries, slot s of head h in page p at
     row (p * heads + h) * page + s (``decode`` reads them)."""
 
-    __slots__ = ("k", "v", "pages", "heads", "dim", "page", "_c")
+    __slots__ = ("k", "v", "pages", "heads", "dim", "page", "_c", "_device")
 
     def __init__(self, k, v, pages, heads, dim, page):
         self.k, self.v = k, v
@@ -451,6 +451,7 @@ class KVCache:
         ps = [_params(c.q, c.k, c.base, c.decoder, mult=c.mult) for c in (k, v)]
         self._c = _KVCache(*ps, *(t.data_ptr() for c in (k, v) for t in (c.codes, c.beta, c.scales)),
                            pages, heads, dim, page, 0)
+        self._device = k.codes.get_device()       # its index, -1: not on a GPU
 
 
 def kv_cache(pages=None, heads=8, dim=128, page=64, q=14, k=4, base=None, decoder=DECODER_FULL,
@@ -481,6 +482,8 @@ def kv_cache(pages=None, heads=8, dim=128, page=64, q=14, k=4, base=None, decode
         for t, n in zip(pools, (nb, nw, 1, nb, nw, 1)):
             if t.numel() != rows * n or not t.is_contiguous() or t.element_size() != 4:
                 raise ValueError("pools must be contiguous 32-bit arrays of the cache's sizes")
+            if t.device != pools[0].device:
+                raise ValueError("pools must be on one device")
         for t in (pools[2], pools[5]):
             if t.dtype != torch.float32:
                 raise ValueError("scales must be float32")
@@ -493,17 +496,25 @@ def kv_cache(pages=None, heads=8, dim=128, page=64, q=14, k=4, base=None, decode
     return KVCache(*coded, pages, heads, dim, page)
 
 
-def _heads(x, name):
+def _pools_device(cache):
+    """The index of the GPU that a cache's pools are on."""
+    if cache._device < 0:
+        raise ValueError("the cache's pools are not on a GPU")
+    return cache._device
+
+
+def _heads(x, name, device):
     """A tokens x heads x dim tensor as the library takes it."""
     s = x.stride()
-    if len(s) != 3 or s[2] != 1 or not x.is_cuda:
-        raise ValueError(f"{name} must be a tokens x heads x dim cuda tensor with unit last stride")
+    if len(s) != 3 or s[2] != 1 or x.get_device() != device:
+        raise ValueError(f"{name} must be a tokens x heads x dim tensor with unit last stride on the "
+                         "cache's GPU")
     return _Heads(x.data_ptr(), s[0], s[1])
 
 
-def _index(x, n, dtype, name):
-    if x.dtype != dtype or x.numel() != n or not x.is_contiguous() or not x.is_cuda:
-        raise ValueError(f"{name} must be a contiguous {dtype} cuda tensor of {n} entries")
+def _index(x, n, dtype, name, device):
+    if x.dtype != dtype or x.numel() != n or not x.is_contiguous() or x.get_device() != device:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} entries on the cache's GPU")
     return x.data_ptr()
 
 
@@ -519,6 +530,7 @@ def kv_append(cache, q, k, v, slots, positions=None, cos=None, sin=None, pairs="
     token; ``pairs``: "halves" or "neighbours") and, with ``hadamard``, by H / sqrt(dim); keys
     and values are coded as ``encode`` codes rows.  ``out`` may have another type than q."""
     import torch
+    device = _pools_device(cache)
     tokens, heads, dim = k.shape
     if heads != cache.heads or dim != cache.dim or v.shape != k.shape:
         raise ValueError("k and v must be tokens x heads x dim of the cache")
@@ -529,15 +541,15 @@ def kv_append(cache, q, k, v, slots, positions=None, cos=None, sin=None, pairs="
         if cos is None or sin is None or positions is None:
             raise ValueError("cos, sin and positions go together")
         for t in (cos, sin):
-            if t.dim() != 2 or t.dtype != torch.float32 or not t.is_contiguous() or not t.is_cuda:
-                raise ValueError("cos and sin must be contiguous 2-D float32 cuda tensors")
+            if t.dim() != 2 or t.dtype != torch.float32 or not t.is_contiguous() or t.get_device() != device:
+                raise ValueError("cos and sin must be contiguous 2-D float32 tensors on the cache's GPU")
         if sin.shape != cos.shape:
             raise ValueError("cos and sin differ in shape")
         rows, rot = cos.shape
         rot *= 2
     for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
         if t is not None:
-            _index(t, dim, torch.float32, name)
+            _index(t, dim, torch.float32, name, device)
     prep = _KVPrep(cos.data_ptr() if rot else None, sin.data_ptr() if rot else None,
                    None if q_norm is None else q_norm.data_ptr(),
                    None if k_norm is None else k_norm.data_ptr(), float(eps), rows, rot,
@@ -552,11 +564,11 @@ def kv_append(cache, q, k, v, slots, positions=None, cos=None, sin=None, pairs="
             out = torch.empty(tokens, q_heads, dim, dtype=q.dtype, device=q.device)
         elif out.shape != q.shape:
             raise ValueError("out must have q's shape")
-        hq, ho = _heads(q, "q"), _heads(out, "out")
+        hq, ho = _heads(q, "q", device), _heads(out, "out", device)
     _check(library().nq_kv_append(
-        cache._c, prep, tokens, _index(slots, tokens, torch.int64, "slots"),
-        _index(positions, tokens, torch.int32, "positions") if rot else None, _dtype_code(k.dtype),
-        hq, q_heads, _heads(k, "k"), _heads(v, "v"), ho,
+        cache._c, prep, tokens, _index(slots, tokens, torch.int64, "slots", device),
+        _index(positions, tokens, torch.int32, "positions", device) if rot else None, _dtype_code(k.dtype),
+        hq, q_heads, _heads(k, "k", device), _heads(v, "v", device), ho,
         _dtype_code(out.dtype) if q is not None else NQ_F32, _stream(stream)))
     return out if q is not None else None
 
@@ -584,13 +596,15 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
     Returns out (q's shape and type); ``lse`` (tokens x query heads float32), if given,
     receives the logarithms of the softmax sums."""
     import torch
+    device = _pools_device(cache)
     tokens, q_heads, dim = q.shape
     if dim != cache.dim:
         raise ValueError("q must be tokens x query heads x dim of the cache")
     seqs = lengths.numel()
-    if table.dim() != 2 or table.shape[0] != seqs or table.dtype != torch.int32 or not table.is_cuda \
-            or (table.shape[1] > 0 and table.stride(1) != 1):
-        raise ValueError("table must be a sequences x pages int32 cuda tensor with unit last stride")
+    if table.dim() != 2 or table.shape[0] != seqs or table.dtype != torch.int32 \
+            or table.get_device() != device or (table.shape[1] > 0 and table.stride(1) != 1):
+        raise ValueError("table must be a sequences x pages int32 tensor with unit last stride on the "
+                         "cache's GPU")
     if starts is None:
         if tokens != seqs:
             raise ValueError("without starts there is one query a sequence")
@@ -607,7 +621,9 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and type")
     if lse is not None:
-        _index(lse, tokens * q_heads, torch.float32, "lse")
+        _index(lse, tokens * q_heads, torch.float32, "lse", device)
+    if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on the cache's GPU")
     lib = library()
     need = lib.nq_attend_workspace_size(cache.heads, dim, tokens, q_heads, seqs, max_queries,
                                         max_length, window, sinks)
@@ -619,9 +635,9 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
             workspace.record_stream(stream)       # freed on return, in use on `stream`
     _check(lib.nq_attend(
         cache._c, table.data_ptr(), table.stride(0) if seqs > 1 else max(table.shape[1], 1),
-        _index(lengths, seqs, torch.int32, "lengths"), seqs,
-        None if starts is None else _index(starts, seqs + 1, torch.int32, "starts"), max_queries,
+        _index(lengths, seqs, torch.int32, "lengths", device), seqs,
+        None if starts is None else _index(starts, seqs + 1, torch.int32, "starts", device), max_queries,
         max_length, window, sinks, dim ** -0.5 if scale is None else scale, _dtype_code(q.dtype),
-        _heads(q, "q"), tokens, q_heads, _heads(out, "out"), None if lse is None else lse.data_ptr(),
+        _heads(q, "q", device), tokens, q_heads, _heads(out, "out", device), None if lse is None else lse.data_ptr(),
         workspace.data_ptr() if need > 0 else None, need, _stream(stream)))
     return out

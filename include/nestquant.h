@@ -350,7 +350,8 @@ typedef struct {
  *             q_heads = 0: no queries (q, q_out ignored).  q_out may be q where the types and
  *             strides are the same, and must not overlap anything else;
  *   k, v      heads rows a token.
- * tokens == 0 is a no-op. */
+ * tokens == 0 is a no-op.  A launch holds fewer than 2^26 workgroups of 256 blocks of keys or
+ * values: calls of more are NQ_ERR_UNSUPPORTED. */
 nq_status nq_kv_append(const nq_kv_cache* cache, const nq_kv_prep* prep, int64_t tokens,
                        const int64_t* slots, const int32_t* positions, nq_dtype dtype,
                        const nq_heads* q, int32_t q_heads, const nq_heads* k, const nq_heads* v,
@@ -384,7 +385,10 @@ nq_status nq_kv_append(const nq_kv_cache* cache, const nq_kv_prep* prep, int64_t
  *   lse       device, tokens x q_heads floats, or NULL;
  *   workspace device, 16-byte aligned, at least nq_attend_workspace_size(...) bytes of scratch,
  *             used until the call's kernels finish on hip_stream.
- * The result is the same from run to run.  tokens == 0 or seqs == 0 is a no-op. */
+ * The result is the same from run to run.  tokens == 0 or seqs == 0 is a no-op.  A launch holds
+ * fewer than 2^24 workgroups, one for every 16 to 128 query rows of a KV head that max_queries
+ * allows each sequence and chunk of its tokens, and one for every 64 of the tokens that a sequence
+ * with more than 64 rows may see: bounds that ask for more are NQ_ERR_UNSUPPORTED. */
 nq_status nq_attend(const nq_kv_cache* cache, const int32_t* table, int64_t table_stride,
                     const int32_t* lengths, int64_t seqs, const int32_t* starts,
                     int64_t max_queries, int64_t max_length, int64_t window, int64_t sinks,

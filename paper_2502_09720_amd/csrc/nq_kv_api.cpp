@@ -21,6 +21,7 @@ nq_status done(hipError_t e, const char* who) {
 }
 
 constexpr int64_t kMaxTokens = (int64_t)1 << 31;
+constexpr int64_t kMaxThreads = (int64_t)1 << 32;   // of a launch (a HIP grid counts them in 32 bits)
 
 nq_status check_cache(const nq_kv_cache* c, const char* who) {
   if (!c) return set_error(NQ_ERR_INVALID_ARG, "%s: cache is NULL", who);
@@ -187,6 +188,12 @@ nq_status nq_kv_append(const nq_kv_cache* cache, const nq_kv_prep* prep, int64_t
   if (q_heads < 0 || tokens < 0 || tokens >= kMaxTokens || tokens * cache->heads >= kMaxTokens ||
       tokens * q_heads >= kMaxTokens)
     return set_error(NQ_ERR_INVALID_ARG, "%s: tokens times heads outside [0, 2^31)", who);
+  // 256 blocks a workgroup of 64 threads, queries beside keys and values up to 2^23 blocks
+  const int64_t nb = cache->dim / 8, q_blocks = tokens * q_heads * nb;
+  const int64_t wgs = 2 * ((tokens * cache->heads * nb + 255) / 256) +
+                      (q_blocks < (int64_t)1 << 23 ? (q_blocks + 255) / 256 : 0);
+  if (wgs * 64 >= kMaxThreads)
+    return set_error(NQ_ERR_UNSUPPORTED, "%s: more workgroups than a launch holds", who);
   if (tokens == 0) return done(hipSuccess, who);
   if (!slots || (prep->rot > 0 && !positions))
     return set_error(NQ_ERR_INVALID_ARG, "%s: slots or positions is NULL", who);
@@ -293,8 +300,10 @@ nq_status nq_attend(const nq_kv_cache* cache, const int32_t* table, int64_t tabl
   a.records = static_cast<unsigned char*>(workspace) + p.part;
   a.groups = p.groups;
   const int64_t wgs = (int64_t)p.chunks * p.blocks * cache->heads * seqs;
-  if (std::max({wgs, (int64_t)p.groups * cache->heads * seqs,
-                (int64_t)p.rows * p.blocks * cache->heads * seqs}) >= kMaxTokens)
+  const int64_t parts = (int64_t)p.rows * p.blocks * cache->heads * seqs;   // rows that are joined
+  const int64_t joins = p.chunks > 1 ? parts / (1024 / cache->dim) + 1 : 0;
+  if (std::max({wgs, (int64_t)p.groups * cache->heads * seqs, joins}) * 256 >= kMaxThreads ||
+      parts >= kMaxTokens)
     return set_error(NQ_ERR_UNSUPPORTED, "%s: more workgroups than a launch holds", who);
   a.mirror = p.chunks == 1 && p.blocks % 2 == 0 && wgs <= 512;
   a.k_scale = (float)(scale * 1.4426950408889634 * cache->k.base * 4.0);

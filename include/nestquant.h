@@ -374,7 +374,8 @@ nq_status nq_kv_append(const nq_kv_cache* cache, const nq_kv_prep* prep, int64_t
  *             (query b belongs to sequence b; tokens = seqs);
  *   max_queries, max_length  upper bounds, known on the host, of the queries of a sequence and of
  *             lengths (queries and tokens past them are not computed and not seen);
- *             max_length <= table_stride * page, max_length < 2^30;
+ *             max_queries <= tokens (unless tokens == 0), max_length <= table_stride * page,
+ *             max_length < 2^30;
  *   window, sinks  >= 0;  scale: finite;
  *   dtype     type of q and out.  Scores, softmax and sums are fp32 and the decoded values exact
  *             integers; 16-bit queries are taken as they are, fp32 ones to 22 bits of the

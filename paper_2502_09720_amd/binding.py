@@ -577,7 +577,7 @@ def attend_workspace_size(cache, tokens, q_heads, seqs, max_queries=1, max_lengt
                           sinks=0):
     """Scratch bytes that ``attend`` needs for calls up to these sizes."""
     n = library().nq_attend_workspace_size(cache.heads, cache.dim, tokens, q_heads, seqs,
-                                           max_queries, max_length, window, sinks)
+                                           min(max_queries, tokens), max_length, window, sinks)
     if n < 0:
         raise ValueError("invalid attend shape")
     return n
@@ -609,7 +609,7 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
         if tokens != seqs:
             raise ValueError("without starts there is one query a sequence")
         max_queries = 1
-    elif max_queries is None:
+    elif max_queries is None or max_queries > tokens:
         max_queries = tokens
     most = table.shape[1] * cache.page
     if max_length is None:

@@ -103,7 +103,8 @@ nq_status check_attend(int32_t heads, int32_t dim, int64_t tokens, int32_t q_hea
     return set_error(NQ_ERR_INVALID_ARG, "%s: tokens * q_heads outside [0, 2^31)", who);
   if (seqs < 0 || seqs > 65535)
     return set_error(NQ_ERR_INVALID_ARG, "%s: seqs=%lld outside [0, 65535]", who, (long long)seqs);
-  if (max_queries < 0 || max_queries > tokens)
+  // a call of no tokens is a no-op whatever its bounds allow
+  if (max_queries < 0 || (tokens > 0 && max_queries > tokens))
     return set_error(NQ_ERR_INVALID_ARG, "%s: max_queries outside [0, tokens]", who);
   if (max_length < 0 || max_length >= ((int64_t)1 << 30))
     return set_error(NQ_ERR_INVALID_ARG, "%s: max_length outside [0, 2^30)", who);

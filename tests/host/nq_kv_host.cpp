@@ -143,8 +143,24 @@ static void launches() {
   CHECK(append(((int64_t)1 << 28) - 8, 1, 256, 7) == NQ_OK);      // the queries in a launch of their own
 }
 
+// No tokens and no sequences: nothing to do, whatever the bounds.
+static void nothing() {
+  Attend a;
+  a = {.seqs = 0, .tokens = 0, .queries = 1, .starts = false};
+  CHECK(a() == NQ_OK && g_calls.empty());
+  a = {.seqs = 3, .tokens = 0, .queries = 4};
+  CHECK(a() == NQ_OK && g_calls.empty());
+  CHECK(nq_attend_workspace_size(8, 128, 0, 32, 0, 1, 100, 0, 0) == 0);
+  CHECK(nq_attend_workspace_size(8, 128, 0, 32, 3, 4, 100, 0, 0) == 0);
+  a = {.seqs = 3, .tokens = 3, .queries = 4};
+  CHECK(a() == NQ_ERR_INVALID_ARG && g_calls.empty());
+  a = {.seqs = 0, .tokens = 0, .queries = -1};
+  CHECK(a() == NQ_ERR_INVALID_ARG && g_calls.empty());
+}
+
 int main() {
   launches();
+  nothing();
   if (g_fail) return 1;
   std::puts("all host KV cache checks passed");
   return 0;

@@ -255,6 +255,7 @@ struct AttendPlan {
   int tiles;             // 16-row tiles of a row block; 0: many rows, decoded records
   int units;             // 16-token tiles of a step
   int blocks, rows, chunks, steps, groups;
+  bool fits;             // whether a launch holds its workgroups; nothing below is set otherwise
   int64_t part;          // bytes of the partial results, which come first in the workspace
   int64_t records;       // bytes of the decoded records
 };

@@ -136,7 +136,6 @@ nq::AttendPlan nq::attend_plan(int heads, int dim, int64_t tokens, int q_heads, 
   const int64_t wgs = std::max<int64_t>(seqs * heads * p.blocks, 1);
   if (p.tiles == 0) {
     p.groups = (int)std::max<int64_t>(tiles(64, max_queries), 1);
-    p.records = seqs * heads * p.groups * (int64_t)(dim * 256 + 1024);
     const int64_t steps = std::max<int64_t>(tiles(64, queries), 1);
     const int64_t chunks = std::max<int64_t>(std::min((512 + wgs - 1) / wgs, (steps + 7) / 8), 1);
     p.steps = (int)((steps + chunks - 1) / chunks);
@@ -155,7 +154,13 @@ nq::AttendPlan nq::attend_plan(int heads, int dim, int64_t tokens, int q_heads, 
     p.steps = (p.steps + 3) / 4 * 4;
     p.chunks = (int)((steps + p.steps - 1) / p.steps);
   }
-  p.part = p.chunks > 1 ? wgs * p.rows * p.chunks * (int64_t)(dim + 4) * 4 : 0;
+  const int64_t records = seqs * heads * p.groups;       // one a workgroup
+  const int64_t parts = wgs * p.rows;                    // rows that are joined, some a workgroup
+  const int64_t joins = p.chunks > 1 ? parts / (1024 / dim) + 1 : 0;
+  p.fits = std::max({wgs * p.chunks, records, joins}) * 256 < kMaxThreads && parts < kMaxTokens;
+  if (!p.fits) return p;
+  p.records = records * (dim * 256 + 1024);
+  p.part = p.chunks > 1 ? parts * p.chunks * (dim + 4) * 4 : 0;
   return p;
 }
 
@@ -247,7 +252,7 @@ int64_t nq_attend_workspace_size(int32_t heads, int32_t dim, int64_t tokens, int
   if (tokens == 0 || seqs == 0 || max_queries == 0) return 0;
   const nq::AttendPlan p = nq::attend_plan(heads, dim, tokens, q_heads, seqs, max_queries,
                                            max_length, window, sinks);
-  return p.part + p.records;
+  return p.fits ? p.part + p.records : -1;
 }
 
 nq_status nq_attend(const nq_kv_cache* cache, const int32_t* table, int64_t table_stride,
@@ -278,6 +283,8 @@ nq_status nq_attend(const nq_kv_cache* cache, const int32_t* table, int64_t tabl
   if (nq_status s = check_rows(out, dtype, "out", who)) return s;
   const nq::AttendPlan p = nq::attend_plan(cache->heads, cache->dim, tokens, q_heads, seqs,
                                            max_queries, max_length, window, sinks);
+  if (!p.fits)
+    return set_error(NQ_ERR_UNSUPPORTED, "%s: more workgroups than a launch holds", who);
   const int64_t need = p.part + p.records;
   if (workspace_bytes < need || (need > 0 && (!workspace || !aligned16(workspace))))
     return set_error(NQ_ERR_INVALID_ARG, "%s: workspace of %lld bytes needed, 16-byte aligned", who,
@@ -301,11 +308,6 @@ nq_status nq_attend(const nq_kv_cache* cache, const int32_t* table, int64_t tabl
   a.records = static_cast<unsigned char*>(workspace) + p.part;
   a.groups = p.groups;
   const int64_t wgs = (int64_t)p.chunks * p.blocks * cache->heads * seqs;
-  const int64_t parts = (int64_t)p.rows * p.blocks * cache->heads * seqs;   // rows that are joined
-  const int64_t joins = p.chunks > 1 ? parts / (1024 / cache->dim) + 1 : 0;
-  if (std::max({wgs, (int64_t)p.groups * cache->heads * seqs, joins}) * 256 >= kMaxThreads ||
-      parts >= kMaxTokens)
-    return set_error(NQ_ERR_UNSUPPORTED, "%s: more workgroups than a launch holds", who);
   a.mirror = p.chunks == 1 && p.blocks % 2 == 0 && wgs <= 512;
   a.k_scale = (float)(scale * 1.4426950408889634 * cache->k.base * 4.0);
   a.v_scale = (float)(cache->v.base * 4.0);

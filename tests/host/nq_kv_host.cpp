@@ -89,6 +89,12 @@ static nq_kv_cache cache(int heads = 8, int dim = 128) {
   return c;
 }
 
+// The size query of a call's arguments.
+static int64_t size(int heads, int dim, int q_heads, int64_t seqs, int64_t tokens, int64_t queries, int64_t length,
+                    int64_t window = 0, int64_t sinks = 0) {
+  return nq_attend_workspace_size(heads, dim, tokens, q_heads, seqs, queries, length, window, sinks);
+}
+
 struct Attend {
   int heads = 8, dim = 128, q_heads = 32;
   int64_t seqs = 1, tokens = 1, queries = 1, length = 100;
@@ -143,6 +149,16 @@ static void launches() {
   CHECK(append(((int64_t)1 << 28) - 8, 1, 256, 7) == NQ_OK);      // the queries in a launch of their own
 }
 
+// The size query refuses what the call refuses, however large.
+static void sizes() {
+  CHECK(size(8, 128, 32, 2048, 32768, 32768, 64) == -1);
+  CHECK(size(8, 128, 32, 2047, 32768, 32768, 64) > 0);
+  CHECK(size(8, 128, 32, 16384, 16384, 1, 128 * 512) == -1);
+  CHECK(size(1024, 256, 1024, 65535, 65535, 65, (1 << 30) - 1) == -1);
+  CHECK(size(1024, 256, 16384, 65535, 65535, 4, (1 << 30) - 1) == -1);
+  CHECK(size(1, 256, 1, 65535, 65535, 65535, (1 << 30) - 1) == -1);
+}
+
 // No tokens and no sequences: nothing to do, whatever the bounds.
 static void nothing() {
   Attend a;
@@ -160,6 +176,7 @@ static void nothing() {
 
 int main() {
   launches();
+  sizes();
   nothing();
   if (g_fail) return 1;
   std::puts("all host KV cache checks passed");

@@ -398,10 +398,18 @@ nq_status nq_attend(const nq_kv_cache* cache, const int32_t* table, int64_t tabl
                     int64_t workspace_bytes, void* hip_stream);
 
 /* Scratch bytes of nq_attend for a cache of `heads` heads of `dim` entries (-1 for sizes it
- * refuses). */
+ * refuses).  They are those of exactly these arguments: a smaller call, which is split along the
+ * cache where a larger one has rows enough, may need more. */
 int64_t nq_attend_workspace_size(int32_t heads, int32_t dim, int64_t tokens, int32_t q_heads,
                                  int64_t seqs, int64_t max_queries, int64_t max_length,
                                  int64_t window, int64_t sinks);
+
+/* Scratch bytes that serve every call of at most these tokens, seqs, max_queries, max_length and
+ * sinks, and of this window or a smaller one (0: any): a workspace to keep (-1 for sizes that
+ * nq_attend refuses).  It grows with every argument. */
+int64_t nq_attend_workspace_bound(int32_t heads, int32_t dim, int64_t tokens, int32_t q_heads,
+                                  int64_t seqs, int64_t max_queries, int64_t max_length,
+                                  int64_t window, int64_t sinks);
 
 /* Statistics for choosing the beta set (App. F): for n sample 8-vectors v (normalized as
  * Alg. 3 normalizes rows, i.e. x / r) and m candidate betas, the squared error of coding

@@ -103,8 +103,9 @@ def library():
         lib.nq_attend.argtypes = [kvp, vp, i64, vp, i64, vp, i64, i64, i64, i64, ctypes.c_double,
                                   ctypes.c_int, hp, i64, i32, hp, vp, vp, i64, vp]
         lib.nq_attend.restype = ctypes.c_int
-        lib.nq_attend_workspace_size.argtypes = [i32, i32, i64, i32, i64, i64, i64, i64, i64]
-        lib.nq_attend_workspace_size.restype = i64
+        for f in (lib.nq_attend_workspace_size, lib.nq_attend_workspace_bound):
+            f.argtypes = [i32, i32, i64, i32, i64, i64, i64, i64, i64]
+            f.restype = i64
         for f in ("nq_encode", "nq_decode", "nq_matmul", "nq_matmul_ex", "nq_matmul_stages"):
             getattr(lib, f).restype = ctypes.c_int
         lib.nq_codes_words.argtypes = [i64, i64]
@@ -575,9 +576,10 @@ def kv_append(cache, q, k, v, slots, positions=None, cos=None, sin=None, pairs="
 
 def attend_workspace_size(cache, tokens, q_heads, seqs, max_queries=1, max_length=1, window=0,
                           sinks=0):
-    """Scratch bytes that ``attend`` needs for calls up to these sizes."""
-    n = library().nq_attend_workspace_size(cache.heads, cache.dim, tokens, q_heads, seqs,
-                                           min(max_queries, tokens), max_length, window, sinks)
+    """Scratch bytes that serve every ``attend`` of at most these sizes, and of this window or a
+    smaller one (nq_attend_workspace_bound): a workspace to keep."""
+    n = library().nq_attend_workspace_bound(cache.heads, cache.dim, tokens, q_heads, seqs,
+                                            min(max_queries, tokens), max_length, window, sinks)
     if n < 0:
         raise ValueError("invalid attend shape")
     return n
@@ -593,6 +595,8 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
     its position, with ``window`` > 0 the last ``window`` of them and the first ``sinks``.
     ``max_queries`` and ``max_length`` bound the queries and the tokens of a sequence (None: as
     many as q and the table allow, at the cost of scratch memory and of idle workgroups).
+    ``workspace``: scratch memory of ``attend_workspace_size`` bytes (a call with less, or None,
+    takes its own from torch's allocator).
     Returns out (q's shape and type); ``lse`` (tokens x query heads float32), if given,
     receives the logarithms of the softmax sums."""
     import torch

@@ -113,6 +113,19 @@ nq_status check_attend(int32_t heads, int32_t dim, int64_t tokens, int32_t q_hea
   return NQ_OK;
 }
 
+// Tiles of `size` tokens that n consecutive queries may see.  It grows with every argument (window
+// 0 counting as the largest) but size.
+int64_t seen_tiles(int64_t size, int64_t n, int64_t max_length, int64_t window, int64_t sinks) {
+  const int64_t whole = (max_length + size - 1) / size;
+  if (window == 0) return whole;
+  const int64_t w = std::min(window, max_length), s = std::min(sinks, max_length);
+  return std::min(whole, (w + n) / size + 2 + (s + size - 1) / size);
+}
+
+// Bytes of a partial row (the maximum, the sum, two unused floats, dim entries) and of a record.
+int64_t part_bytes(int dim) { return (int64_t)(dim + 4) * 4; }
+int64_t record_bytes(int dim) { return (int64_t)dim * 256 + 1024; }
+
 }  // namespace
 
 nq::AttendPlan nq::attend_plan(int heads, int dim, int64_t tokens, int q_heads, int64_t seqs,
@@ -125,13 +138,7 @@ nq::AttendPlan nq::attend_plan(int heads, int dim, int64_t tokens, int q_heads, 
   const int64_t most = p.tiles == 0 ? 128 : 16 * p.tiles;
   p.blocks = (int)((rows + most - 1) / most);
   p.rows = (int)std::min(rows, most);
-  // tiles of `size` tokens that n consecutive queries may see
-  auto tiles = [&](int64_t size, int64_t n) {
-    const int64_t whole = (max_length + size - 1) / size;
-    if (window == 0) return whole;
-    const int64_t w = std::min(window, max_length), s = std::min(sinks, max_length);
-    return std::min(whole, (w + n) / size + 2 + (s + size - 1) / size);
-  };
+  auto tiles = [&](int64_t size, int64_t n) { return seen_tiles(size, n, max_length, window, sinks); };
   const int64_t queries = std::min(max_queries, most / group + 2);   // of a row block
   const int64_t wgs = std::max<int64_t>(seqs * heads * p.blocks, 1);
   if (p.tiles == 0) {
@@ -159,8 +166,8 @@ nq::AttendPlan nq::attend_plan(int heads, int dim, int64_t tokens, int q_heads, 
   const int64_t joins = p.chunks > 1 ? parts / (1024 / dim) + 1 : 0;
   p.fits = std::max({wgs * p.chunks, records, joins}) * 256 < kMaxThreads && parts < kMaxTokens;
   if (!p.fits) return p;
-  p.records = records * (dim * 256 + 1024);
-  p.part = p.chunks > 1 ? parts * p.chunks * (dim + 4) * 4 : 0;
+  p.records = records * record_bytes(dim);
+  p.part = p.chunks > 1 ? parts * p.chunks * part_bytes(dim) : 0;
   return p;
 }
 
@@ -253,6 +260,42 @@ int64_t nq_attend_workspace_size(int32_t heads, int32_t dim, int64_t tokens, int
   const nq::AttendPlan p = nq::attend_plan(heads, dim, tokens, q_heads, seqs, max_queries,
                                            max_length, window, sinks);
   return p.fits ? p.part + p.records : -1;
+}
+
+// What no plan of smaller arguments exceeds.  The sizes themselves are not monotone: fewer rows or
+// sequences are split into more chunks, and a chunk's steps are rounded.
+int64_t nq_attend_workspace_bound(int32_t heads, int32_t dim, int64_t tokens, int32_t q_heads,
+                                  int64_t seqs, int64_t max_queries, int64_t max_length,
+                                  int64_t window, int64_t sinks) {
+  if (check_attend(heads, dim, tokens, q_heads, seqs, max_queries, max_length, window, sinks,
+                   "nq_attend_workspace_bound"))
+    return -1;
+  if (tokens == 0 || seqs == 0 || max_queries == 0) return 0;
+  if (!nq::attend_plan(heads, dim, tokens, q_heads, seqs, max_queries, max_length, window, sinks).fits)
+    return -1;
+  const int64_t group = q_heads / heads, rows = max_queries * group, pairs = seqs * heads;
+  int64_t few = 0, many = 0;
+  {
+    // Few rows: at most 64 a pair, in blocks of 16 or 32 (padded to 32 from 17 on); chunks n with
+    //   blocks pairs n <= max(2048 + blocks pairs, blocks pairs ceil(steps / 16)),
+    // n <= ceil(tiles / 4), and one where there are no more than eight tiles.
+    const int64_t r = std::min<int64_t>(rows, 64), block = dim < 256 ? 32 : 16;
+    const int64_t padded = r <= 16 ? r : (r + 31) / 32 * 32, blocks = (r + 15) / 16;
+    const int64_t all = seen_tiles(16, std::min(max_queries, 32 / group + 2), max_length, window, sinks);
+    const int64_t wgs = pairs * blocks, chunks = (all + 3) / 4;
+    if (all > 8)
+      few = std::min(std::max(2048 + wgs, wgs * (((all + 1) / 2 + 15) / 16)) * std::min(r, block),
+                     pairs * padded * chunks);
+  }
+  if (rows > 64) {
+    // Many: blocks of 128 rows; more than one chunk below 512 blocks and above 8 records only.
+    const int64_t wgs = std::min<int64_t>(pairs * ((rows + 127) / 128), 511);
+    const int64_t steps = seen_tiles(64, std::min(max_queries, 128 / group + 2), max_length, window, sinks);
+    if (steps > 8) many = std::min(511 + wgs, wgs * ((steps + 7) / 8)) * std::min<int64_t>(rows, 128);
+  }
+  const int64_t records =
+      rows > 64 ? pairs * std::max<int64_t>(seen_tiles(64, max_queries, max_length, window, sinks), 1) : 0;
+  return std::max(few * part_bytes(dim), many * part_bytes(dim) + records * record_bytes(dim));
 }
 
 nq_status nq_attend(const nq_kv_cache* cache, const int32_t* table, int64_t table_stride,

@@ -4,8 +4,11 @@
 // pointer is read.
 //
 // Exit status 0 when every check passes; each failure prints its line.
+#include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <random>
 #include <string>
 #include <vector>
 
@@ -159,6 +162,49 @@ static void sizes() {
   CHECK(size(1, 256, 1, 65535, 65535, 65535, (1 << 30) - 1) == -1);
 }
 
+// A workspace of the bound serves every smaller call, and the bound stays near the size.
+static void bounds() {
+  std::mt19937_64 rng(1);
+  auto up_to = [&](int64_t most) {   // spread over the logarithm, 0 and the largest now and then
+    if (rng() % 8 == 0) return rng() % 2 ? most : (int64_t)0;
+    const double x = std::exp(std::log((double)most + 1) * ((double)(rng() >> 11) * 0x1p-53));
+    return std::min((int64_t)x, most);
+  };
+  int compared = 0;
+  for (int i = 0; i < 400000; ++i) {
+    const int dims[] = {64, 128, 256}, groups[] = {1, 2, 3, 4, 5, 8, 12, 16, 17, 40};
+    const int dim = dims[rng() % 3], heads = 1 + (int)up_to(15), q_heads = heads * groups[rng() % 10];
+    const int64_t tokens = up_to(40000), seqs = up_to(300), queries = up_to(tokens), length = up_to(300000);
+    const int64_t window = rng() % 2 ? 0 : up_to(5000), sinks = up_to(300);
+    const int64_t bound = nq_attend_workspace_bound(heads, dim, tokens, q_heads, seqs, queries, length, window, sinks);
+    const int64_t own = size(heads, dim, q_heads, seqs, tokens, queries, length, window, sinks);
+    CHECK((bound < 0) == (own < 0));
+    CHECK(bound >= own);
+    if (bound < 0) continue;
+    // beside the records: 1022 workgroups of 128 rows, or 2048 and four a pair and 512 tokens of 32
+    CHECK(bound <= own + (1022 * 128 + 2048 * 32 + seqs * heads * 4 * (2 + length / 512) * 32) * 4 * (dim + 4));
+    for (int j = 0; j < 8; ++j) {
+      const int64_t t = up_to(tokens), w = window ? std::max<int64_t>(up_to(window), 1) : up_to(5000);
+      const int64_t s = up_to(seqs), q = up_to(std::min(t, queries)), l = up_to(length), k = up_to(sinks);
+      const int64_t smaller = size(heads, dim, q_heads, s, t, q, l, w, k);
+      if (smaller < 0) continue;
+      if (smaller > bound) {
+        std::fprintf(stderr, "%d heads of %d, %d query heads: %lld of %lld for tokens %lld/%lld seqs %lld/%lld "
+                     "queries %lld/%lld length %lld/%lld window %lld/%lld sinks %lld/%lld\n", heads, dim, q_heads,
+                     (long long)smaller, (long long)bound, (long long)t, (long long)tokens, (long long)s,
+                     (long long)seqs, (long long)q, (long long)queries, (long long)l, (long long)length,
+                     (long long)w, (long long)window, (long long)k, (long long)sinks);
+        ++g_fail;
+        return;
+      }
+      ++compared;
+      const int64_t b = nq_attend_workspace_bound(heads, dim, t, q_heads, s, q, l, w, k);
+      CHECK(b <= bound);
+    }
+  }
+  CHECK(compared > 1000000);
+}
+
 // No tokens and no sequences: nothing to do, whatever the bounds.
 static void nothing() {
   Attend a;
@@ -177,6 +223,7 @@ static void nothing() {
 int main() {
   launches();
   sizes();
+  bounds();
   nothing();
   if (g_fail) return 1;
   std::puts("all host KV cache checks passed");

@@ -27,3 +27,26 @@ def test_more_queries_allowed_than_there_are(nq):
     c = Call(nq, 700, [90, 40], [1, 2], dtype="f32")
     assert torch.equal(c.run(max_queries=50), c.run(max_queries=3))
     c.check(max_queries=50)
+
+
+def test_one_workspace_for_smaller_calls(nq):
+    """A workspace of the largest call's size is the one that smaller calls use, whether they are
+    split more or less: nothing is allocated beside it."""
+    import torch
+    heads, group, dim, most = 8, 4, 128, 2049
+    calls = [([2049], [1]), ([2048], [1]), ([300], [1]), ([2048], [17]), ([2040], [40]), ([1500], [300]),
+             ([129], [2])]
+    ws = None
+    for i, (lengths, counts) in enumerate(calls):
+        c = Call(nq, 710 + i, lengths, counts, heads=heads, group=group, dim=dim, page=64, dtype="f32")
+        if ws is None:
+            need = nq.attend_workspace_size(c.cache, 300, heads * group, 1, max_queries=300, max_length=most)
+            ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+        up = lambda a: torch.from_numpy(a).cuda()
+        args = (c.cache, c.q, up(c.table), up(c.lengths))
+        more = dict(starts=up(c.starts), max_queries=counts[0], max_length=lengths[0], out=torch.empty_like(c.q),
+                    workspace=ws)
+        before = torch.cuda.memory_stats()["allocation.all.allocated"]
+        got = nq.attend(*args, **more)
+        assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
+        assert torch.equal(got, c.run())

@@ -519,6 +519,17 @@ def _index(x, n, dtype, name, device):
     return x.data_ptr()
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory for a call on ``stream``: from that stream's own pool, so that what is still to run on
+    the current stream with memory it freed is not written over, and memory freed while the call
+    runs is handed out again behind it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def kv_append(cache, q, k, v, slots, positions=None, cos=None, sin=None, pairs="halves",
               q_norm=None, k_norm=None, eps=1e-5, hadamard=True, out=None, stream=None):
     """nq_kv_append: codes the keys and values of new tokens (tokens x heads x dim cuda tensors
@@ -529,7 +540,8 @@ def kv_append(cache, q, k, v, slots, positions=None, cos=None, sin=None, pairs="
     Queries and keys are normed (``q_norm``, ``k_norm``: dim float32 weights), rotated by
     position (``cos``, ``sin``: positions x rot / 2 float32 tables, ``positions`` int32, one a
     token; ``pairs``: "halves" or "neighbours") and, with ``hadamard``, by H / sqrt(dim); keys
-    and values are coded as ``encode`` codes rows.  ``out`` may have another type than q."""
+    and values are coded as ``encode`` codes rows.  ``out`` may have another type than q.  With
+    ``stream``, a new output belongs to that stream's memory."""
     import torch
     device = _pools_device(cache)
     tokens, heads, dim = k.shape
@@ -562,7 +574,7 @@ def kv_append(cache, q, k, v, slots, positions=None, cos=None, sin=None, pairs="
             raise ValueError("q must be tokens x query heads x dim")
         q_heads = q.shape[1]
         if out is None:
-            out = torch.empty(tokens, q_heads, dim, dtype=q.dtype, device=q.device)
+            out = _empty((tokens, q_heads, dim), q.dtype, q.device, stream)
         elif out.shape != q.shape:
             raise ValueError("out must have q's shape")
         hq, ho = _heads(q, "q", device), _heads(out, "out", device)
@@ -621,7 +633,7 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
     elif max_length > most:
         raise ValueError("max_length exceeds the table's pages")
     if out is None:
-        out = torch.empty(tokens, q_heads, dim, dtype=q.dtype, device=q.device)
+        out = _empty((tokens, q_heads, dim), q.dtype, q.device, stream)
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and type")
     if lse is not None:
@@ -634,9 +646,7 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
     if need < 0:
         raise ValueError("invalid attend shape")
     if need > 0 and (workspace is None or workspace.numel() * workspace.element_size() < need):
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        if stream is not None:
-            workspace.record_stream(stream)       # freed on return, in use on `stream`
+        workspace = _empty((need,), torch.uint8, q.device, stream)
     _check(lib.nq_attend(
         cache._c, table.data_ptr(), table.stride(0) if seqs > 1 else max(table.shape[1], 1),
         _index(lengths, seqs, torch.int32, "lengths", device), seqs,

@@ -338,7 +338,8 @@ typedef struct {
 
 /* Appends tokens to a cache: every key row through prep's steps and every value row as it is is
  * coded (as nq_encode codes a row, bit for bit) straight into its slot, and every query row goes
- * through prep's steps into q_out.  One launch, no workspace.
+ * through prep's steps into q_out.  No workspace; one launch, or two where the queries have 2^23
+ * blocks of 8 entries or more.
  *   tokens    new tokens, of any sequences; tokens * q_heads < 2^31;
  *   slots     device, tokens int64: token i goes to slot slots[i] % page of page
  *             slots[i] / page; a slot outside [0, pages * page) (such as -1) leaves the

@@ -1,5 +1,6 @@
 // Appending to a coded KV cache (nq_kv_append): the rows of new queries, keys and values from
-// the projections to where attention reads them, in one launch.
+// the projections to where attention reads them, in one launch (queries of many million blocks have
+// one of their own).
 //
 // A lane holds one 8-entry block and a row of NB = dim / 8 blocks takes NB lanes of a wave, so
 // every step stays in registers: the norm's sum of squares goes across the lanes of a row by

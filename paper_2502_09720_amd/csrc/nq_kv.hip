@@ -107,9 +107,12 @@ struct RowSteps {
       s = wave_sum<NB>(s);
       // 1 / sqrt(mean + eps) in fp64: two Newton steps from the hardware's reciprocal root
       const double x = s * (1.0 / (8 * NB)) + a.eps;
+      // (which is right by itself where the mean is infinite or 0)
       double y = __builtin_amdgcn_rsq(x);
-      y = __builtin_fma(0.5 * y, __builtin_fma(-x * y, y, 1.0), y);
-      y = __builtin_fma(0.5 * y, __builtin_fma(-x * y, y, 1.0), y);
+      if (x > 0.0 && x < INFINITY) {
+        y = __builtin_fma(0.5 * y, __builtin_fma(-x * y, y, 1.0), y);
+        y = __builtin_fma(0.5 * y, __builtin_fma(-x * y, y, 1.0), y);
+      }
       const float f = (float)y;
 #pragma unroll
       for (int l = 0; l < 8; ++l) v[l] = (v[l] * f) * w[l];

@@ -510,7 +510,8 @@ def _heads(x, name, device):
     if len(s) != 3 or s[2] != 1 or x.get_device() != device:
         raise ValueError(f"{name} must be a tokens x heads x dim tensor with unit last stride on the "
                          "cache's GPU")
-    return _Heads(x.data_ptr(), s[0], s[1])
+    # the stride of a single token or head steps nowhere, whatever it is
+    return _Heads(x.data_ptr(), s[0] if x.shape[0] != 1 else 0, s[1] if x.shape[1] != 1 else 0)
 
 
 def _index(x, n, dtype, name, device):

@@ -1,0 +1,35 @@
+"""Views that torch makes of a serving program's tensors, as arguments of kv_append and attend."""
+
+import pytest
+
+from test_gpu_attend import nq  # noqa: F401 (the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def test_strides_of_a_single_token_or_head(nq):
+    """A dimension of one entry may have any stride: a token of a row of odd width, a head alone."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    lengths, table = torch.tensor([5], dtype=torch.int32, device="cuda"), torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    slot = torch.tensor([4], device="cuda")
+    for heads in (2, 1):
+        caches = [nq.kv_cache(1, heads, 64, 16) for _ in range(2)]
+        past = rand(4, heads, 64)
+        for c in caches:
+            nq.kv_append(c, None, past, past, torch.arange(4, device="cuda"))
+        wide = rand(3, (4 * heads + 2 * heads) * 64 + 3)          # rows 3 entries past the heads
+        rows = wide[1:2, :-3]
+        outs = []
+        # the odd width makes the second row start off the alignment: take it from an aligned copy
+        aligned = torch.empty(rows.numel() + 3, dtype=rows.dtype, device="cuda")
+        odd = aligned.as_strided(rows.shape, (rows.numel() + 3, 1)).copy_(rows)
+        for c, x in ((caches[0], rows.contiguous()), (caches[1], odd)):
+            q, k, v = x.unflatten(1, (6 * heads, 64)).split((4 * heads, heads, heads), 1)
+            if heads == 1 and x is odd:
+                k, v = (t.as_strided(t.shape, (t.stride(0), 7, 1)) for t in (k, v))
+            q = nq.kv_append(c, q, k, v, slot)
+            one = q if x is not odd else q.as_strided(q.shape, (1, *q.stride()[1:]))
+            outs.append(nq.attend(c, one, table, lengths))
+        assert torch.equal(*outs)

@@ -628,6 +628,9 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
         max_queries = 1
     elif max_queries is None or max_queries > tokens:
         max_queries = tokens
+    if seqs > 1 and table.stride(0) < table.shape[1]:      # rows that overlap, as an expanded row's
+        with torch.cuda.stream(stream):
+            table = table.contiguous()
     most = table.shape[1] * cache.page
     if max_length is None:
         max_length = most

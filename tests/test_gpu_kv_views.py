@@ -33,3 +33,22 @@ def test_strides_of_a_single_token_or_head(nq):
             one = q if x is not odd else q.as_strided(q.shape, (1, *q.stride()[1:]))
             outs.append(nq.attend(c, one, table, lengths))
         assert torch.equal(*outs)
+
+
+def test_one_table_row_for_all_sequences(nq):
+    """Sequences over the same pages, their table an expanded row."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(2)
+    cache = nq.kv_cache(8, 2, 64, 16)
+    k, v = (torch.randn(100, 2, 64, generator=g, device="cuda") for _ in range(2))
+    nq.kv_append(cache, None, k, v, torch.arange(100, device="cuda"))
+    q = torch.randn(3, 4, 64, generator=g, device="cuda")
+    lengths = torch.tensor([100, 77, 3], dtype=torch.int32, device="cuda")
+    row = torch.arange(8, dtype=torch.int32, device="cuda").view(1, 8)
+    want = nq.attend(cache, q, row.repeat(3, 1), lengths)
+    assert torch.equal(nq.attend(cache, q, row.expand(3, -1), lengths), want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = nq.attend(cache, q, row.expand(3, -1), lengths, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want)

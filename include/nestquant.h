@@ -274,7 +274,9 @@ nq_status nq_encode_matmul(int32_t flags, const nq_params* pa, const void* x, nq
  * pages * heads * page rows of dim entries, stored as every coded matrix of the library
  * (nq_decode reads them as they are):
  * slot s of head h in page p is row (p * heads + h) * page + s.
- *   k, v     quantizer parameters of the keys and of the values (First-beta);
+ *   k, v     quantizer parameters of the keys and of the values (First-beta).  nq_attend reads
+ *            caches of one decoder: with different ones the pools can be filled and decoded, but
+ *            attention over them is NQ_ERR_UNSUPPORTED;
  *   dim      entries of a head: 64, 128 or 256;
  *   page     tokens of a page: 16, 32, 64, 128 or 256;
  *   pages    pages of a pool; pages * page < 2^40;

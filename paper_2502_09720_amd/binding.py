@@ -460,9 +460,10 @@ def kv_cache(pages=None, heads=8, dim=128, page=64, q=14, k=4, base=None, decode
     """A coded KV cache of ``pages`` pages of ``page`` tokens (16, 32, 64, 128 or 256) of
     ``heads`` heads of ``dim`` entries (64, 128 or 256).  q, k, base, decoder and mult are the
     quantizer's parameters (as ``encode``) for the keys and, unless ``values`` (a dict of the
-    same) says otherwise, the values.  ``pools``: the six arrays (codes, beta words and scales of
-    the keys, then of the values) of the caller, contiguous, instead of new ones, whose scales
-    are zero; the cache then has as many pages as they hold."""
+    same) says otherwise, the values; ``attend`` needs one decoder for both.  ``pools``: the six
+    arrays (codes, beta words and scales of the keys, then of the values) of the caller,
+    contiguous, instead of new ones, whose scales are zero; the cache then has as many pages as
+    they hold."""
     import torch
     if dim < 8 or dim % 8 or heads < 1 or page < 1:
         raise ValueError("invalid cache shape")
@@ -540,9 +541,9 @@ def kv_append(cache, q, k, v, slots, positions=None, cos=None, sin=None, pairs="
 
     Queries and keys are normed (``q_norm``, ``k_norm``: dim float32 weights), rotated by
     position (``cos``, ``sin``: positions x rot / 2 float32 tables, ``positions`` int32, one a
-    token; ``pairs``: "halves" or "neighbours") and, with ``hadamard``, by H / sqrt(dim); keys
-    and values are coded as ``encode`` codes rows.  ``out`` may have another type than q.  With
-    ``stream``, a new output belongs to that stream's memory."""
+    token, not read without tables; ``pairs``: "halves" or "neighbours") and, with ``hadamard``,
+    by H / sqrt(dim); keys and values are coded as ``encode`` codes rows.  ``out`` may have another
+    type than q.  With ``stream``, a new output belongs to that stream's memory."""
     import torch
     device = _pools_device(cache)
     tokens, heads, dim = k.shape

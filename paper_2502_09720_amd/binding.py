@@ -498,21 +498,15 @@ def kv_cache(pages=None, heads=8, dim=128, page=64, q=14, k=4, base=None, decode
     return KVCache(*coded, pages, heads, dim, page)
 
 
-def _pools_device(cache):
-    """The index of the GPU that a cache's pools are on."""
-    if cache._device < 0:
-        raise ValueError("the cache's pools are not on a GPU")
-    return cache._device
-
-
 def _heads(x, name, device):
     """A tokens x heads x dim tensor as the library takes it."""
     s = x.stride()
     if len(s) != 3 or s[2] != 1 or x.get_device() != device:
         raise ValueError(f"{name} must be a tokens x heads x dim tensor with unit last stride on the "
                          "cache's GPU")
-    # the stride of a single token or head steps nowhere, whatever it is
-    return _Heads(x.data_ptr(), s[0] if x.shape[0] != 1 else 0, s[1] if x.shape[1] != 1 else 0)
+    if (s[0] | s[1]) & 7:       # the stride of a single token or head steps nowhere, whatever it is
+        s = [0 if n == 1 else step for n, step in zip(x.shape, s)]
+    return _Heads(x.data_ptr(), s[0], s[1])
 
 
 def _index(x, n, dtype, name, device):
@@ -545,7 +539,9 @@ def kv_append(cache, q, k, v, slots, positions=None, cos=None, sin=None, pairs="
     by H / sqrt(dim); keys and values are coded as ``encode`` codes rows.  ``out`` may have another
     type than q.  With ``stream``, a new output belongs to that stream's memory."""
     import torch
-    device = _pools_device(cache)
+    device = cache._device
+    if device < 0:
+        raise ValueError("the cache's pools are not on a GPU")
     tokens, heads, dim = k.shape
     if heads != cache.heads or dim != cache.dim or v.shape != k.shape:
         raise ValueError("k and v must be tokens x heads x dim of the cache")
@@ -614,13 +610,17 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
     Returns out (q's shape and type); ``lse`` (tokens x query heads float32), if given,
     receives the logarithms of the softmax sums."""
     import torch
-    device = _pools_device(cache)
+    device = cache._device
+    if device < 0:
+        raise ValueError("the cache's pools are not on a GPU")
     tokens, q_heads, dim = q.shape
     if dim != cache.dim:
         raise ValueError("q must be tokens x query heads x dim of the cache")
     seqs = lengths.numel()
-    if table.dim() != 2 or table.shape[0] != seqs or table.dtype != torch.int32 \
-            or table.get_device() != device or (table.shape[1] > 0 and table.stride(1) != 1):
+    ok = table.dim() == 2 and table.dtype == torch.int32 and table.get_device() == device
+    if ok:
+        (rows, pages), (step, unit) = table.shape, table.stride()
+    if not ok or rows != seqs or (pages > 0 and unit != 1):
         raise ValueError("table must be a sequences x pages int32 tensor with unit last stride on the "
                          "cache's GPU")
     if starts is None:
@@ -629,10 +629,12 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
         max_queries = 1
     elif max_queries is None or max_queries > tokens:
         max_queries = tokens
-    if seqs > 1 and table.stride(0) < table.shape[1]:      # rows that overlap, as an expanded row's
-        with torch.cuda.stream(stream):
-            table = table.contiguous()
-    most = table.shape[1] * cache.page
+    if seqs == 1 or step < pages:
+        step = pages
+        if seqs > 1:                     # rows that overlap, as an expanded row's
+            with torch.cuda.stream(stream):
+                table = table.contiguous()
+    most = pages * cache.page
     if max_length is None:
         max_length = most
     elif max_length > most:
@@ -653,7 +655,7 @@ def attend(cache, q, table, lengths, starts=None, max_queries=None, max_length=N
     if need > 0 and (workspace is None or workspace.numel() * workspace.element_size() < need):
         workspace = _empty((need,), torch.uint8, q.device, stream)
     _check(lib.nq_attend(
-        cache._c, table.data_ptr(), table.stride(0) if seqs > 1 else max(table.shape[1], 1),
+        cache._c, table.data_ptr(), max(step, 1),
         _index(lengths, seqs, torch.int32, "lengths", device), seqs,
         None if starts is None else _index(starts, seqs + 1, torch.int32, "starts", device), max_queries,
         max_length, window, sinks, dim ** -0.5 if scale is None else scale, _dtype_code(q.dtype),

@@ -19,13 +19,11 @@ def test_strides_of_a_single_token_or_head(nq):
         past = rand(4, heads, 64)
         for c in caches:
             nq.kv_append(c, None, past, past, torch.arange(4, device="cuda"))
-        wide = rand(3, (4 * heads + 2 * heads) * 64 + 3)          # rows 3 entries past the heads
-        rows = wide[1:2, :-3]
+        rows = rand(1, 6 * heads * 64)
+        odd = rand(1, 6 * heads * 64 + 3)[:, :-3]                # a row 3 entries wider than the heads
+        odd.copy_(rows)
         outs = []
-        # the odd width makes the second row start off the alignment: take it from an aligned copy
-        aligned = torch.empty(rows.numel() + 3, dtype=rows.dtype, device="cuda")
-        odd = aligned.as_strided(rows.shape, (rows.numel() + 3, 1)).copy_(rows)
-        for c, x in ((caches[0], rows.contiguous()), (caches[1], odd)):
+        for c, x in ((caches[0], rows), (caches[1], odd)):
             q, k, v = x.unflatten(1, (6 * heads, 64)).split((4 * heads, heads, heads), 1)
             if heads == 1 and x is odd:
                 k, v = (t.as_strided(t.shape, (t.stride(0), 7, 1)) for t in (k, v))

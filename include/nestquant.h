@@ -381,8 +381,8 @@ nq_status nq_kv_append(const nq_kv_cache* cache, const nq_kv_prep* prep, int64_t
  *             max_length < 2^30;
  *   window, sinks  >= 0;  scale: finite;
  *   dtype     type of q and out.  Scores, softmax and sums are fp32 and the decoded values exact
- *             integers; 16-bit queries are taken as they are, fp32 ones to 22 bits of the
- *             row's largest entry; the softmax's weights, times their values' scales, to 22
+ *             integers; 16-bit queries are taken as they are (to 2^-39 of the row's largest
+ *             entry), fp32 ones to 22 bits of the row's largest entry; the softmax's weights, times their values' scales, to 22
  *             bits or 2^-37 of the largest such product among the tokens that the row sees
  *             (weights below 2^-76 of the row's largest may count as 0);
  *   q, out    tokens x q_heads rows; out must not overlap q;

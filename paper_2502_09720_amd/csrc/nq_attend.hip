@@ -19,9 +19,9 @@
 //
 // The waves' results are joined in LDS, the chunks' by join_kernel, in a fixed order.
 //
-// What bounds it: vector instructions, about 2080 a step of 32 tokens and wave, of which 16 blocks a
-// lane take 105 each; 0.96 a clock of a busy CU.  131072 tokens of 8 KV heads: 124 us (1.2 TB/s of
-// codes, a quarter of what a copy reaches); 64 ragged sequences of up to 8192: 299 us.  Three
+// What bounds it: vector instructions, about 2040 a step of 32 tokens and wave, of which 16 blocks a
+// lane take 105 each; 0.98 a clock of a busy CU.  131072 tokens of 8 KV heads: 123 us (1.2 TB/s of
+// codes, a quarter of what a copy reaches); 64 ragged sequences of up to 8192: 290-298 us.  Three
 // waves a SIMD without scratch beat four with it (250 against 280 us at 32 x 8192 tokens).
 #include <type_traits>
 

@@ -11,8 +11,9 @@
 //
 // What bounds it: at one token the chain of dependent steps of a wave (7 us), at thousands the
 // encoder's vector instructions for keys and values (720 a wave of 64 blocks with norm and
-// rotations, 0.98 a clock of a busy CU: 90-97 us for 16384 tokens of 8 heads) and memory for the
-// queries (64 heads of them: 115-124 us, 4.3 TB/s).
+// rotations, 0.97 a clock of a busy CU: 91-104 us for 16384 tokens of 8 heads); the queries are at
+// the limits of both memory and vector issue (64 heads of them: 115-128 us, 4.2-4.7 TB/s, 1.01
+// vector instructions a clock of a busy CU).
 #include <type_traits>
 
 #include "nq_encode_block.hpp"

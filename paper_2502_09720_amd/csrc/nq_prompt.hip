@@ -21,8 +21,8 @@
 //
 // What bounds it: per 64 tokens and 32 rows a wave issues 48 matrix instructions (1536 clocks of its
 // SIMD at DIM = 128), about 220 vector instructions and 32 exponentials (1400) and reads 32 KiB
-// of LDS; two waves a SIMD overlap them in part.  8192 queries of 32 heads: 800 us, 687 TFLOP/s;
-// 2048: 90 us, where one round of workgroups with 1 to 32 records each is the limit.
+// of LDS; two waves a SIMD overlap them in part.  8192 queries of 32 heads: 800-823 us, 668-687
+// TFLOP/s; 2048: 83-91 us, where one round of workgroups with 1 to 32 records each is the limit.
 #include <type_traits>
 
 #include "nq_attend.hpp"

@@ -379,12 +379,13 @@ nq_status nq_kv_append(const nq_kv_cache* cache, const nq_kv_prep* prep, int64_t
  *             lengths (queries and tokens past them are not computed and not seen);
  *             max_queries <= tokens (unless tokens == 0), max_length <= table_stride * page,
  *             max_length < 2^30;
- *   window, sinks  >= 0;  scale: finite;
+ *   window, sinks  >= 0;  scale: finite, also times 4 log2(e) base of the keys in fp32;
  *   dtype     type of q and out.  Scores, softmax and sums are fp32 and the decoded values exact
  *             integers; 16-bit queries are taken as they are (to 2^-39 of the row's largest
- *             entry), fp32 ones to 22 bits of the row's largest entry; the softmax's weights, times their values' scales, to 22
- *             bits or 2^-37 of the largest such product among the tokens that the row sees
- *             (weights below 2^-76 of the row's largest may count as 0);
+ *             entry), fp32 ones to 22 bits of the row's largest entry; the softmax's weights,
+ *             times their values' scales, to 22 bits or 2^-37 of the largest such product among
+ *             the tokens that the row sees (weights below 2^-76 of the row's largest may count
+ *             as 0);
  *   q, out    tokens x q_heads rows; out must not overlap q;
  *   lse       device, tokens x q_heads floats, or NULL;
  *   workspace device, 16-byte aligned, at least nq_attend_workspace_size(...) bytes of scratch,

@@ -312,7 +312,9 @@ nq_status nq_attend(const nq_kv_cache* cache, const int32_t* table, int64_t tabl
   if (nq_status s = check_attend(cache->heads, cache->dim, tokens, q_heads, seqs, max_queries,
                                  max_length, window, sinks, who))
     return s;
-  if (!std::isfinite(scale)) return set_error(NQ_ERR_INVALID_ARG, "%s: scale is not finite", who);
+  const float k_scale = (float)(scale * 1.4426950408889634 * cache->k.base * 4.0);
+  if (!std::isfinite(scale) || !std::isfinite(k_scale))
+    return set_error(NQ_ERR_INVALID_ARG, "%s: scale is not finite in fp32", who);
   if (table_stride < 0 || max_length > table_stride * cache->page)
     return set_error(NQ_ERR_INVALID_ARG, "%s: max_length exceeds table_stride * page", who);
   if (cache->pages >= kMaxTokens)
@@ -352,7 +354,7 @@ nq_status nq_attend(const nq_kv_cache* cache, const int32_t* table, int64_t tabl
   a.groups = p.groups;
   const int64_t wgs = (int64_t)p.chunks * p.blocks * cache->heads * seqs;
   a.mirror = p.chunks == 1 && p.blocks % 2 == 0 && wgs <= 512;
-  a.k_scale = (float)(scale * 1.4426950408889634 * cache->k.base * 4.0);
+  a.k_scale = k_scale;
   a.v_scale = (float)(cache->v.base * 4.0);
   a.seqs = (int)seqs;
   a.tokens = (int)tokens;

@@ -102,12 +102,13 @@ struct Attend {
   int heads = 8, dim = 128, q_heads = 32;
   int64_t seqs = 1, tokens = 1, queries = 1, length = 100;
   bool starts = true;
+  double scale = 0.1;
   nq_status operator()() const {
     g_calls.clear();
     const nq_kv_cache c = cache(heads, dim);
     const nq_heads x = {DEV, (int64_t)q_heads * dim, dim};
     return nq_attend(&c, static_cast<int32_t*>(DEV), 1 << 20, static_cast<int32_t*>(DEV), seqs,
-                     starts ? static_cast<int32_t*>(DEV) : nullptr, queries, length, 0, 0, 0.1, NQ_BF16, &x,
+                     starts ? static_cast<int32_t*>(DEV) : nullptr, queries, length, 0, 0, scale, NQ_BF16, &x,
                      tokens, q_heads, &x, nullptr, DEV, (int64_t)1 << 60, nullptr);
   }
 };
@@ -220,8 +221,19 @@ static void nothing() {
   CHECK(a() == NQ_ERR_INVALID_ARG && g_calls.empty());
 }
 
+// The scale reaches the kernels in fp32.
+static void scales() {
+  Attend a;
+  a = {.scale = 1e38};
+  CHECK(a() == NQ_OK && std::isfinite(g_attend.k_scale));
+  a = {.scale = -1e40};
+  CHECK(a() == NQ_ERR_INVALID_ARG && g_calls.empty());
+  CHECK(g_error.find("nq_attend: scale") == 0);
+}
+
 int main() {
   launches();
+  scales();
   sizes();
   bounds();
   nothing();
